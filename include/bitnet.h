@@ -488,6 +488,82 @@ bitnet_status bitnet_linear_fused_segmented(const void* x, bitnet_dtype x_dtype,
 bitnet_status bitnet_unpack_weights(const void* packed, int64_t N, int64_t K, bitnet_format f,
                                     int8_t* codes, void* stream);
 
+/*
+ * The attention half of a decoder layer (Section 2, "LLaMA-alike components": rotary positions and causal attention stand between
+ * the merged Q | K | V BitLinear and the output BitLinear): keys and values in a paged cache, and the attention that reads it.
+ *
+ * The cache: two buffers of bitnet_kv_cache_bytes() bytes, bf16.  A page holds page_tokens tokens (a multiple of 32) of every key-value
+ * head, as blocks of 32 tokens; with Dp = 8*ceil(head_dim/8) a block has 32*Dp elements, and block i of head h on page p starts at
+ * element ((p*kv_heads + h)*(page_tokens/32) + i) * 32*Dp of its buffer.  So a page is one piece of either buffer.
+ *   keys    [Dp/8][32][8]: 8 consecutive dims of a token together; token t of the block stands at place
+ *           16*((t>>2)&1) + 4*(t>>3) + (t&3) of the 32 -- the order in which the rows of an MFMA operand tile become the next product's
+ *           operand without moving between lanes.  Dims head_dim .. Dp-1 are zeros (bitnet_rope_kv_append writes them).
+ *   values  [4][Dp][8]: 8 consecutive tokens of a dim together, token t at [t>>3][d][t&7].
+ *
+ * bitnet_kv (host, read during the call) names the cache and which sequences use it:
+ *   k, v             the two buffers, 16-byte aligned
+ *   pages, page_tokens, kv_heads, head_dim    the cache's shape; head_dim even, 2 ... 256
+ *   sequences        their number B
+ *   page_table       [B] rows of max_pages int32 (device), table_stride elements apart: the page of position pos of sequence b is
+ *                    page_table[b*table_stride + pos/page_tokens].  Entries behind a sequence's length are not used.
+ *   kv_len           [B] int32 (device): tokens of the sequence, those of the call included.  Lengths outside 0 ... max_pages*page_tokens
+ *                    count as the nearest of the two.
+ *   q_start          [B+1] int32 (device), not falling: rows q_start[b] .. q_start[b+1]-1 of the call are the last tokens of sequence b, so
+ *                    row r has position kv_len[b] - q_start[b+1] + r.  Rows in front of q_start[0] and from q_start[B] on are left alone.
+ *                    NULL: one row for each sequence, row b at position kv_len[b] - 1.
+ *   A table entry that names no page of the cache (outside 0 ... pages-1) is a page that is not there: tokens on it are not stored, and are no
+ *   keys.  A row at a negative position is stored nowhere and sees no key; its attention is zeros.  Pages may be shared by sequences that
+ *   only read them; two rows of one call that are stored at one place leave either of them there.
+ * Limits: pages*kv_heads*page_tokens/32 < 2^31; max_pages*page_tokens < 2^31 - 64; fewer than 2^31 blocks of 32 tokens in all sequences'
+ * tables together; heads a multiple of kv_heads, up to 16384; at most 2^22 rows, rows*heads < 2^28 and sequences*heads < 2^22.
+ */
+typedef struct bitnet_kv {
+    void* k;
+    void* v;
+    int64_t pages, page_tokens, kv_heads, head_dim;
+    int64_t sequences;
+    const int32_t* page_table;
+    int64_t table_stride, max_pages;
+    const int32_t* kv_len;
+    const int32_t* q_start;
+} bitnet_kv;
+
+/* Bytes of one of the cache's two buffers (host out). */
+bitnet_status bitnet_kv_cache_bytes(int64_t pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, size_t* bytes);
+
+/*
+ * Rotary positions on the queries and keys of a merged projection; keys and values go into the cache, queries come back.
+ *   qkv       [T][(heads + 2 kv_heads)*head_dim] (queries | keys | values), dtype F32 or BF16, element-aligned: what bitnet_linear(_segmented)
+ *             writes for the merged matrix
+ *   inv_freq  [rotary_dims/2] float (device): a pair's angle at position pos is pos*inv_freq[i], taken to a fraction of a turn in fp64
+ *   rotary_dims   the first dims of a head, even, 0 ... head_dim: turned; the others pass unturned.  pairs == 0: dim i goes with dim
+ *             i + rotary_dims/2; otherwise 2i with 2i+1.  (a, b) -> (a cos - b sin, b cos + a sin), in fp32
+ *   T         rows of qkv; == kv->sequences if kv->q_start is NULL (BITNET_ERR_SHAPE otherwise)
+ *   q         out [T][heads][head_dim] BF16, 2-byte aligned; bf16 (round to nearest even) as the cache is
+ * One launch.
+ */
+bitnet_status bitnet_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, const float* inv_freq, int64_t rotary_dims, int pairs,
+                                    const bitnet_kv* kv, int64_t T, int64_t heads, void* q, void* stream);
+
+/*
+ * o = softmax(scale q . k) v over the cached keys and values of each row's sequence; query head i reads key-value head i / (heads/kv_heads).
+ * The row at position pos sees the keys of positions 0 .. pos, whatever memory holds behind them.  Scores, weights' sums and the
+ * sums over values are fp32; weights enter their product as bf16, for an F32 result as the sum of two bf16.
+ *   q          [rows][heads][head_dim] BF16, 2-byte aligned, as bitnet_rope_kv_append writes it
+ *   scale      > 0 and finite (BITNET_ERR_SHAPE otherwise), ordinarily 1/sqrt(head_dim)
+ *   o          out [rows][heads*head_dim], F32 or BF16, element-aligned: what bitnet_quantize_acts or bitnet_linear_fused takes next
+ *   workspace  device memory, 16-byte aligned, or NULL: contents are scratch; calls that share it must not overlap.  With the
+ *              bitnet_attention_workspace() bytes or more, few rows on long sequences are spread over the chip: parts of a sequence are
+ *              summed up by different workgroups and joined by a second launch
+ *   bitnet_attention_decode   one row for each sequence (kv->q_start is not read)
+ *   bitnet_attention_prefill  runs of T rows in all, dealt out by kv->q_start (BITNET_ERR_NULL without)
+ */
+bitnet_status bitnet_attention_workspace(const bitnet_kv* kv, int64_t T, int64_t heads, int prefill, size_t* bytes);
+bitnet_status bitnet_attention_decode(const void* q, const bitnet_kv* kv, int64_t heads, float scale, void* o, bitnet_dtype o_dtype,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+bitnet_status bitnet_attention_prefill(const void* q, const bitnet_kv* kv, int64_t T, int64_t heads, float scale, void* o,
+                                       bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,8 +36,18 @@ SYMBOLS = [
     "bitnet_rmsnorm_linear_fused", "bitnet_rmsnorm_linear_fused_segmented", "bitnet_swiglu_linear_fused",
     "bitnet_ffn_gate_up_fused", "bitnet_linear_workspace", "bitnet_linear_ws", "bitnet_linear_describe",
     "bitnet_entry_describe", "bitnet_abs_sum", "bitnet_quantize_weights_sharded", "bitnet_quantize_weights_static",
-    "bitnet_repack_weights", "bitnet_linear_workspace_format",
+    "bitnet_repack_weights", "bitnet_linear_workspace_format", "bitnet_kv_cache_bytes", "bitnet_rope_kv_append",
+    "bitnet_attention_workspace", "bitnet_attention_decode", "bitnet_attention_prefill",
 ]
+
+
+class KvStruct(ctypes.Structure):
+    """bitnet_kv of bitnet.h."""
+    _fields_ = ([("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+                + [(n, ctypes.c_int64) for n in ("pages", "page_tokens", "kv_heads", "head_dim", "sequences")]
+                + [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                   ("kv_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p)])
+
 
 _lib = None
 _call = None          # the native marshalling of the hot entry points, bound to _lib
@@ -89,6 +99,12 @@ def load():
     lib.bitnet_entry_describe.argtypes = [ci, ci, i64, i64, i64, ci, sz, ctypes.c_char_p, sz]
     lib.bitnet_linear_ws.argtypes = [vp, vp, vp, vp, ci, i64, i64, i64, ci, vp, ci, ci, vp, sz, vp]
     lib.bitnet_ffn_gate_up_fused.argtypes = [vp, ci, ci, vp, ctypes.c_float, vp, vp, ci, i64, i64, i64, ci, vp, ci, vp]
+    kvp, szp = ctypes.POINTER(KvStruct), ctypes.POINTER(sz)
+    lib.bitnet_kv_cache_bytes.argtypes = [i64, i64, i64, i64, szp]
+    lib.bitnet_rope_kv_append.argtypes = [vp, ci, vp, i64, ci, kvp, i64, i64, vp, vp]
+    lib.bitnet_attention_workspace.argtypes = [kvp, i64, i64, ci, szp]
+    lib.bitnet_attention_decode.argtypes = [vp, kvp, i64, ctypes.c_float, vp, ci, vp, sz, vp]
+    lib.bitnet_attention_prefill.argtypes = [vp, kvp, i64, i64, ctypes.c_float, vp, ci, vp, sz, vp]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = ci
     try:
@@ -337,6 +353,47 @@ def ffn_gate_up_fused(x, packed, gamma, F, norm=False, g=None, eps=1e-6, gamma_p
     """h [M,F] = silu(y_gate) * y_up with [y_gate | y_up] = BitLinear(pre(x)) over a merged gate|up matrix [2F,K] in one
     decode launch; pre = RMSNorm (gain g or None, eps) when norm, else the plain absmax quantization."""
     return _native().ffn_gate_up_fused(x, packed, gamma, F, norm, g, eps, gamma_per_block, fmt, h_dtype, h)
+
+
+def kv_cache(pages, page_tokens, kv_heads, head_dim, device="cuda"):
+    """A paged key-value cache, zeros: (k_cache [pages, kv_heads, page_tokens / 32, Dp / 8, 32, 8], v_cache [..., 4, Dp, 8]), bfloat16, Dp
+    being head_dim rounded up to 8; bitnet.h has the places of the elements.  A page is a row of either tensor."""
+    lib = load()
+    out = ctypes.c_size_t(0)
+    _check(lib.bitnet_kv_cache_bytes(pages, page_tokens, kv_heads, head_dim, ctypes.byref(out)), "bitnet_kv_cache_bytes")
+    blocks, Dp = page_tokens // 32, (head_dim + 7) // 8 * 8
+    return (torch.zeros((pages, kv_heads, blocks, Dp // 8, 32, 8), dtype=torch.bfloat16, device=device),
+            torch.zeros((pages, kv_heads, blocks, 4, Dp, 8), dtype=torch.bfloat16, device=device))
+
+
+def rope_kv_append(qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_start=None, pairs=False, q=None):
+    """The rows of a merged Q | K | V product [T, (heads + 2 kv heads) D] (fp32 / bf16) at their positions: rotary on queries and keys (inv_freq
+    float32 [dims / 2] or None), keys and values into the cache -> queries, bfloat16 [T, heads, D].  kv_len counts each sequence's
+    tokens with the new ones; q_start [B + 1] deals out the rows, None: one row per sequence."""
+    return _native().rope_kv_append(qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_start, pairs, q)
+
+
+def attention_workspace(T, heads, head_dim, k_cache, page_table, prefill=False):
+    """Bytes of scratch with which attention_decode (or attention_prefill) may spread few rows on long sequences over the chip (0: none)."""
+    lib = load()
+    one = 16                                   # stands for the device pointers, which the query does not read
+    kv = KvStruct(one, one, k_cache.shape[0], 32 * k_cache.shape[2], k_cache.shape[1], head_dim, page_table.shape[0], one, page_table.shape[1],
+                  page_table.shape[1], one, one if prefill else None)
+    out = ctypes.c_size_t(0)
+    _check(lib.bitnet_attention_workspace(ctypes.byref(kv), T, heads, int(prefill), ctypes.byref(out)), "bitnet_attention_workspace")
+    return int(out.value)
+
+
+def attention_decode(q, k_cache, v_cache, page_table, kv_len, scale=None, y_dtype=BF16, y=None, workspace=None):
+    """Attention of one new token per sequence, q [B, heads, D] bfloat16, over its cached keys and values -> y [B, heads D].  scale None:
+    1 / sqrt(D); workspace None: one is allocated where it is of use."""
+    return _native().attention_decode(q, k_cache, v_cache, page_table, kv_len, None, scale, y_dtype, y, workspace)
+
+
+def attention_prefill(q, k_cache, v_cache, page_table, kv_len, q_start, scale=None, y_dtype=BF16, y=None, workspace=None):
+    """Causal attention of runs of new tokens, q [T, heads, D] bfloat16 dealt out by q_start [B + 1], over their sequences' caches, which hold
+    the new tokens already -> y [T, heads D]."""
+    return _native().attention_prefill(q, k_cache, v_cache, page_table, kv_len, q_start, scale, y_dtype, y, workspace)
 
 
 def unpack_weights(packed, N, K, fmt=PACK_2BIT, codes=None):

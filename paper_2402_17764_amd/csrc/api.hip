@@ -4,7 +4,9 @@
 
 #include "bitnet_device.hpp"
 #include "bitnet_internal.hpp"
+#include "kv_layout.hpp"
 
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -38,6 +40,32 @@ bool out_type(bitnet_dtype t, OutType* o) {
         default: break;
     }
     return false;
+}
+
+constexpr int64_t kMaxHeads = 16384, kMaxRows = (int64_t)1 << 22, kMaxBlocks = ((int64_t)1 << 31) - 1;
+// Of these the attention kernels' grids follow: at most a workgroup for 64 query rows and one for each head of each sequence.
+constexpr int64_t kMaxRowHeads = ((int64_t)1 << 28) - 1, kMaxSequenceHeads = ((int64_t)1 << 22) - 1;
+
+bool cache_shape_ok(int64_t pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim) {
+    if (pages <= 0 || page_tokens <= 0 || kv_heads <= 0 || head_dim < 2) return false;
+    if (head_dim > 256 || head_dim % 2 || page_tokens % bitnet::kKvBlock || page_tokens >= ((int64_t)1 << 31) || kv_heads > kMaxHeads) return false;
+    return pages <= kMaxBlocks / (kv_heads * (page_tokens / bitnet::kKvBlock));
+}
+
+// The checks that every call on a cache makes
+bitnet_status kv_view(const bitnet_kv* kv, int64_t rows, int64_t heads, bitnet::KvView* view) {
+    if (!kv || !kv->k || !kv->v || !kv->page_table || !kv->kv_len) return BITNET_ERR_NULL;
+    if (!cache_shape_ok(kv->pages, kv->page_tokens, kv->kv_heads, kv->head_dim)) return BITNET_ERR_SHAPE;
+    const int64_t blocks = kv->page_tokens / bitnet::kKvBlock, B = kv->sequences;
+    if (B <= 0 || rows <= 0 || rows > kMaxRows || heads <= 0 || heads > kMaxHeads || heads % kv->kv_heads) return BITNET_ERR_SHAPE;
+    if (rows > kMaxRowHeads / heads || B > kMaxSequenceHeads / heads) return BITNET_ERR_SHAPE;
+    if (kv->max_pages <= 0 || kv->table_stride < kv->max_pages || kv->table_stride > kMaxElems / B) return BITNET_ERR_SHAPE;
+    if (kv->max_pages > ((((int64_t)1 << 31) - 65) / bitnet::kKvBlock) / blocks || kv->max_pages * blocks > kMaxBlocks / B) return BITNET_ERR_SHAPE;
+    if (!aligned(kv->k, 16) || !aligned(kv->v, 16) || !aligned(kv->page_table, 4) || !aligned(kv->kv_len, 4) || !aligned(kv->q_start, 4))
+        return BITNET_ERR_ALIGN;
+    *view = {static_cast<uint16_t*>(kv->k), static_cast<uint16_t*>(kv->v), kv->page_table, kv->kv_len, kv->q_start, kv->table_stride,
+             (int32_t)kv->pages, (int32_t)blocks, (int32_t)(kv->max_pages * blocks), (int32_t)kv->kv_heads, (int32_t)kv->head_dim, (int32_t)B};
+    return BITNET_OK;
 }
 
 }  // namespace
@@ -572,6 +600,65 @@ bitnet_status bitnet_unpack_weights(const void* packed, int64_t N, int64_t K, bi
     if (f == BITNET_PACK_2BIT)
         return from_hip(bitnet::launch_unpack_2bit(packed, N, K, codes, static_cast<hipStream_t>(stream)));
     return from_hip(bitnet::launch_unpack_trit5(packed, N, K, codes, static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_kv_cache_bytes(int64_t pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim, size_t* bytes) {
+    if (!bytes) return BITNET_ERR_NULL;
+    if (!cache_shape_ok(pages, page_tokens, kv_heads, head_dim)) return BITNET_ERR_SHAPE;
+    *bytes = (size_t)(pages * kv_heads * page_tokens) * (size_t)bitnet::kv_padded_dim((int)head_dim) * 2;
+    return BITNET_OK;
+}
+
+bitnet_status bitnet_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, const float* inv_freq, int64_t rotary_dims, int pairs,
+                                    const bitnet_kv* kv, int64_t T, int64_t heads, void* q, void* stream) {
+    if (!qkv || !q || (!inv_freq && rotary_dims != 0)) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    const bitnet_status st = kv_view(kv, T, heads, &view);
+    if (st != BITNET_OK) return st;
+    if (rotary_dims < 0 || rotary_dims > view.D || rotary_dims % 2 || (!view.q_start && T != view.B)) return BITNET_ERR_SHAPE;
+    if (qkv_dtype != BITNET_F32 && qkv_dtype != BITNET_BF16) return BITNET_ERR_DTYPE;
+    if (!aligned(qkv, dtype_size(qkv_dtype)) || !aligned(q, 2) || !aligned(inv_freq, 4)) return BITNET_ERR_ALIGN;
+    return from_hip(bitnet::launch_rope_append(qkv, qkv_dtype == BITNET_BF16, inv_freq, (int)rotary_dims, pairs != 0, view, T, (int)heads, q,
+                                               static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_attention_workspace(const bitnet_kv* kv, int64_t T, int64_t heads, int prefill, size_t* bytes) {
+    if (!bytes) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    const bitnet_status st = kv_view(kv, T, heads, &view);
+    if (st != BITNET_OK) return st;
+    *bytes = prefill ? bitnet::attention_prefill_workspace_bytes(view, T, (int)heads) : bitnet::attention_decode_workspace_bytes(view, (int)heads);
+    return BITNET_OK;
+}
+
+static bitnet_status attention_checked(const void* q, const bitnet_kv* kv, int64_t T, int64_t heads, float scale, void* o, bitnet_dtype o_dtype,
+                                       void* workspace, bitnet::KvView* view) {
+    if (!q || !o) return BITNET_ERR_NULL;
+    const bitnet_status st = kv_view(kv, T, heads, view);
+    if (st != BITNET_OK) return st;
+    if (!(scale > 0.0f) || !isfinite(scale)) return BITNET_ERR_SHAPE;
+    if (o_dtype != BITNET_F32 && o_dtype != BITNET_BF16) return BITNET_ERR_DTYPE;
+    if (!aligned(q, 2) || !aligned(o, dtype_size(o_dtype)) || !aligned(workspace, 16)) return BITNET_ERR_ALIGN;
+    return BITNET_OK;
+}
+
+bitnet_status bitnet_attention_decode(const void* q, const bitnet_kv* kv, int64_t heads, float scale, void* o, bitnet_dtype o_dtype,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+    bitnet::KvView view;
+    const bitnet_status st = attention_checked(q, kv, kv ? kv->sequences : 1, heads, scale, o, o_dtype, workspace, &view);
+    if (st != BITNET_OK) return st;
+    return from_hip(bitnet::launch_attention_decode(q, view, (int)heads, scale, o, o_dtype == BITNET_F32, workspace,
+                                                    workspace ? workspace_bytes : 0, static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_attention_prefill(const void* q, const bitnet_kv* kv, int64_t T, int64_t heads, float scale, void* o,
+                                       bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    bitnet::KvView view;
+    const bitnet_status st = attention_checked(q, kv, T, heads, scale, o, o_dtype, workspace, &view);
+    if (st != BITNET_OK) return st;
+    if (!view.q_start) return BITNET_ERR_NULL;
+    return from_hip(bitnet::launch_attention_prefill(q, view, T, (int)heads, scale, o, o_dtype == BITNET_F32, workspace,
+                                                     workspace ? workspace_bytes : 0, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -174,4 +174,16 @@ bool gemv_trit5_supports(int64_t M, int64_t N, int64_t K, const void* xq);
 hipError_t launch_linear_gemv_trit5(const int8_t* xq, const float* sx, const void* packed, const float* gamma,
                                     int64_t M, int64_t N, int64_t K, void* y, OutType yt, hipStream_t stream, LaunchPlan* plan = nullptr);
 
+struct KvView;                         // kv_layout.hpp
+// rope_append.hip: rotary positions, keys and values into the paged cache
+hipError_t launch_rope_append(const void* qkv, bool bf16, const float* inv_freq, int rotary, bool pairs, const KvView& kv, int64_t T, int heads,
+                              void* q, hipStream_t stream);
+// attention_decode.hip, attention_prefill.hip; a workspace smaller than its query's bytes is not used
+size_t attention_decode_workspace_bytes(const KvView& kv, int heads);
+hipError_t launch_attention_decode(const void* q, const KvView& kv, int heads, float scale, void* o, bool f32, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+size_t attention_prefill_workspace_bytes(const KvView& kv, int64_t T, int heads);
+hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
 }  // namespace bitnet

@@ -8,7 +8,10 @@
 // around the call, as ctypes does.
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -31,6 +34,10 @@ struct Abi {
     decltype(&bitnet_rmsnorm_linear_fused_segmented) rmsnorm_linear_fused_segmented;
     decltype(&bitnet_swiglu_linear_fused) swiglu_linear_fused;
     decltype(&bitnet_ffn_gate_up_fused) ffn_gate_up_fused;
+    decltype(&bitnet_rope_kv_append) rope_kv_append;
+    decltype(&bitnet_attention_workspace) attention_workspace;
+    decltype(&bitnet_attention_decode) attention_decode;
+    decltype(&bitnet_attention_prefill) attention_prefill;
 } abi;
 PyObject* error_class = nullptr;
 
@@ -376,6 +383,108 @@ ENTRY(ffn_gate_up_fused) {      // x, packed, gamma, F, norm, g, eps, gamma_per_
     });
 }
 
+// The cache and its sequences as the C ABI takes them: k_cache [pages, kv heads, page tokens / 32, Dp / 8, 32, 8] and v_cache [pages, kv heads,
+// page tokens / 32, 4, Dp, 8] (bf16), page_table [B, pages of a sequence] (int32, its rows may be strided), kv_len [B] and q_start [B + 1] or None (int32).
+// Every tensor has to be on x's device, which is the current one while the call lasts.
+struct Cache {
+    const at::Tensor& x;
+    c10::DeviceGuard on;
+    bitnet_kv kv;
+    const at::Tensor& here(PyObject* o, const char* name, at::ScalarType dt) const { return here(tensor(o, name, dt), name); }
+    const at::Tensor& here(const at::Tensor& t, const char* name) const {
+        if (t.device() != x.device()) raise(PyExc_ValueError, "%s is on another device", name);
+        return t;
+    }
+    Cache(const at::Tensor& x_, int64_t head_dim, PyObject* ok, PyObject* ov, PyObject* otable, PyObject* olen, PyObject* ostart) : x(x_), on(x_.device()) {
+        const at::Tensor &k = here(ok, "k_cache", at::kBFloat16), &v = here(ov, "v_cache", at::kBFloat16);
+        const int64_t Dp = (head_dim + 7) / 8 * 8;
+        if (k.dim() != 6 || k.size(3) != Dp / 8 || k.size(4) != 32 || k.size(5) != 8)
+            raise(PyExc_ValueError, "k_cache must be [pages, kv heads, page tokens / 32, %lld, 32, 8] for heads of %lld", (long long)(Dp / 8), (long long)head_dim);
+        if (v.dim() != 6 || v.size(0) != k.size(0) || v.size(1) != k.size(1) || v.size(2) != k.size(2) || v.size(3) != 4 || v.size(4) != Dp || v.size(5) != 8)
+            raise(PyExc_ValueError, "v_cache must be [pages, kv heads, page tokens / 32, 4, %lld, 8], of the pages of k_cache", (long long)Dp);
+        if (!THPVariable_Check(otable) || !THPVariable_Unpack(otable).is_cuda()) raise(PyExc_TypeError, "page_table must be a CUDA/HIP tensor");
+        const at::Tensor& table = here(THPVariable_Unpack(otable), "page_table");
+        if (table.scalar_type() != at::kInt) raise(PyExc_TypeError, "page_table has dtype %s", dtype_name(table.scalar_type()));
+        two_d(table, "page_table");
+        const int64_t B = table.size(0), pages = table.size(1);
+        if ((pages > 1 && table.stride(1) != 1) || (B > 1 && table.stride(0) < pages)) raise(PyExc_ValueError, "page_table must have contiguous rows");
+        const at::Tensor& len = here(olen, "kv_len", at::kInt);
+        if (len.dim() != 1 || len.size(0) != B) raise(PyExc_ValueError, "kv_len must have one entry per row of page_table");
+        const int32_t* start = nullptr;
+        if (ostart != Py_None) {
+            const at::Tensor& t = here(ostart, "q_start", at::kInt);
+            if (t.dim() != 1 || t.size(0) != B + 1) raise(PyExc_ValueError, "q_start must have one entry more than page_table has rows");
+            start = static_cast<const int32_t*>(t.const_data_ptr());
+        }
+        kv = {k.mutable_data_ptr(), v.mutable_data_ptr(), k.size(0), k.size(2) * 32, k.size(1), head_dim, B, static_cast<const int32_t*>(table.const_data_ptr()),
+              B > 1 ? table.stride(0) : pages, pages, static_cast<const int32_t*>(len.const_data_ptr()), start};
+    }
+    at::Tensor output(PyObject* given, const char* name, at::IntArrayRef shape, at::ScalarType dt) const {
+        if (given == Py_None) return at::empty(shape, at::TensorOptions().dtype(dt).device(x.device()));
+        const at::Tensor& t = here(given, name, dt);
+        if (t.sizes() != shape) raise(PyExc_ValueError, "%s has another shape than the result", name);
+        return t;
+    }
+    void* stream() const { return c10::hip::getCurrentHIPStream(x.device().index()).stream(); }
+};
+
+ENTRY(rope_kv_append) {      // qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_start, pairs, q
+    return entry(n, 10, [&] {
+        bitnet_dtype dt;
+        const at::Tensor& qkv = matrix(a[0], "qkv", &dt);
+        const int64_t T = qkv.size(0), heads = integer(a[6]);
+        const at::Tensor& k = tensor(a[2], "k_cache");
+        const int64_t kv_heads = k.dim() == 6 ? k.size(1) : 1;
+        if (heads <= 0 || heads > qkv.size(1) || qkv.size(1) % (heads + 2 * kv_heads) != 0)
+            raise(PyExc_ValueError, "qkv must have the columns of heads queries and two times kv heads keys and values");
+        const int64_t D = qkv.size(1) / (heads + 2 * kv_heads);
+        Cache c(qkv, D, a[2], a[3], a[4], a[5], a[7]);
+        const float* freq = nullptr;
+        int64_t rotary = 0;
+        if (a[1] != Py_None) {
+            const at::Tensor& f = c.here(a[1], "inv_freq", at::kFloat);
+            if (f.dim() != 1) raise(PyExc_ValueError, "inv_freq must be 1-D");
+            freq = static_cast<const float*>(f.const_data_ptr());
+            rotary = 2 * f.size(0);
+        }
+        const int pairs = truth(a[8]) ? 1 : 0;
+        at::Tensor q = c.output(a[9], "q", {T, heads, D}, at::kBFloat16);
+        const void* xp = qkv.const_data_ptr();
+        void *qp = q.mutable_data_ptr(), *st = c.stream();
+        call("bitnet_rope_kv_append", [&] { return abi.rope_kv_append(xp, dt, freq, rotary, pairs, &c.kv, T, heads, qp, st); });
+        return THPVariable_Wrap(q);
+    });
+}
+
+PyObject* attention(PyObject* const* a, bool prefill) {      // q, k_cache, v_cache, page_table, kv_len, q_start, scale, y_dtype, y, workspace
+    const at::Tensor& q = tensor(a[0], "q", at::kBFloat16);
+    if (q.dim() != 3) raise(PyExc_ValueError, "q must be 3-D");
+    const int64_t T = q.size(0), heads = q.size(1), D = q.size(2);
+    Cache c(q, D, a[1], a[2], a[3], a[4], a[5]);
+    if (!prefill && T != c.kv.sequences) raise(PyExc_ValueError, "q must have one row per row of page_table");
+    if (D <= 0) raise(PyExc_ValueError, "q has heads of no dims");
+    const float scale = a[6] == Py_None ? (float)(1.0 / std::sqrt((double)D)) : real(a[6]);
+    const at::ScalarType dt = out_type(a[7]);
+    if (dt == at::kInt) raise(PyExc_ValueError, "y_dtype must be F32 or BF16");
+    at::Tensor y = c.output(a[8], "y", {T, heads * D}, dt), ws;
+    size_t bytes = 0;
+    if (a[9] == Py_None) {
+        call("bitnet_attention_workspace", [&] { return abi.attention_workspace(&c.kv, T, heads, prefill, &bytes); });
+        if (bytes) ws = at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(q.device()));
+    } else {
+        ws = c.here(tensor(a[9], "workspace"), "workspace");
+        bytes = (size_t)ws.numel() * ws.element_size();
+    }
+    void *wp = bytes ? ws.mutable_data_ptr() : nullptr, *yp = y.mutable_data_ptr(), *st = c.stream();
+    const void* qp = q.const_data_ptr();
+    const bitnet_dtype yt = dt == at::kFloat ? BITNET_F32 : BITNET_BF16;
+    if (prefill) call("bitnet_attention_prefill", [&] { return abi.attention_prefill(qp, &c.kv, T, heads, scale, yp, yt, wp, bytes, st); });
+    else call("bitnet_attention_decode", [&] { return abi.attention_decode(qp, &c.kv, heads, scale, yp, yt, wp, bytes, st); });
+    return THPVariable_Wrap(y);
+}
+ENTRY(attention_decode) { return entry(n, 10, [&] { return attention(a, false); }); }
+ENTRY(attention_prefill) { return entry(n, 10, [&] { return attention(a, true); }); }
+
 // bind({name: address}, BitnetError)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *addresses, *cls;
@@ -394,6 +503,7 @@ PyObject* bind(PyObject*, PyObject* args) {
     TAKE(quantize_acts); TAKE(rmsnorm_quantize); TAKE(swiglu_quantize); TAKE(linear); TAKE(linear_variant); TAKE(linear_segmented);
     TAKE(linear_ws); TAKE(linear_fused); TAKE(linear_fused_segmented); TAKE(rmsnorm_linear_fused);
     TAKE(rmsnorm_linear_fused_segmented); TAKE(swiglu_linear_fused); TAKE(ffn_gate_up_fused);
+    TAKE(rope_kv_append); TAKE(attention_workspace); TAKE(attention_decode); TAKE(attention_prefill);
 #undef TAKE
     abi = got;
     Py_INCREF(cls);
@@ -407,6 +517,7 @@ PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
     FAST(quantize_acts), FAST(rmsnorm_quantize), FAST(swiglu_quantize), FAST(linear), FAST(linear_segmented), FAST(linear_ws),
     FAST(linear_fused), FAST(rmsnorm_linear_fused), FAST(swiglu_linear_fused), FAST(ffn_gate_up_fused),
+    FAST(rope_kv_append), FAST(attention_decode), FAST(attention_prefill),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
