@@ -64,7 +64,7 @@ bitnet_status kv_view(const bitnet_kv* kv, int64_t rows, int64_t heads, bitnet::
     if (!aligned(kv->k, 16) || !aligned(kv->v, 16) || !aligned(kv->page_table, 4) || !aligned(kv->kv_len, 4) || !aligned(kv->q_start, 4))
         return BITNET_ERR_ALIGN;
     *view = {static_cast<uint16_t*>(kv->k), static_cast<uint16_t*>(kv->v), kv->page_table, kv->kv_len, kv->q_start, kv->table_stride,
-             (int32_t)kv->pages, (int32_t)blocks, (int32_t)(kv->max_pages * blocks), (int32_t)kv->kv_heads, (int32_t)kv->head_dim, (int32_t)B};
+             (int32_t)kv->pages, (int32_t)blocks, (int32_t)kv->max_pages, (int32_t)(kv->max_pages * blocks), (int32_t)kv->kv_heads, (int32_t)kv->head_dim, (int32_t)B};
     return BITNET_OK;
 }
 

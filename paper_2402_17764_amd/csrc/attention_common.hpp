@@ -10,6 +10,9 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
+// Of a head's kC chunks of 32 dims as the kernels are built (1, 2, 3, 4, 6 or 8), how many are whole for every head that takes them.
+constexpr int whole_chunks(int kC) { return kC <= 4 ? kC - 1 : kC - 2; }
+
 constexpr float kMinusInf = -__builtin_inff();
 
 __device__ inline v4f mfma_bf16(v8bf a, v8bf b, v4f c) {
@@ -66,19 +69,20 @@ __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int
     }
 }
 
-// Eight weights as an operand.  bf16 keeps 8 bits of each: the sums of products then carry a relative error of about 2^-9 / sqrt(keys), which
-// a bf16 result hides.  For a 32-bit result what that rounding left over goes through the product as a second operand.
-__device__ inline v8bf weights_operand(const float (&p)[8]) {
-    v8bf w;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = (__bf16)p[i];
-    return w;
-}
-__device__ inline v8bf weights_rest(const float (&p)[8], v8bf w) {
-    v8bf r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = (__bf16)(p[i] - (float)w[i]);
-    return r;
+// Weights as operands, the pair j, j + 1 of eight.  bf16 keeps 8 bits of each: the sums of products then carry a relative error of about
+// 2^-9 / sqrt(keys), which a bf16 result hides.  For a 32-bit result what that rounding leaves goes through the product too, and what its
+// rounding leaves: three operands hold all 24 bits of a weight (two leave 2^-17 of it: measured 1.3e-6 of the result, three 2e-7).
+template <bool kF32>
+__device__ inline void weights_pair(v8bf* w, int j, float p0, float p1) {
+    w[0][j] = (__bf16)p0;
+    w[0][j + 1] = (__bf16)p1;
+    if (kF32) {
+        const float r0 = p0 - (float)w[0][j], r1 = p1 - (float)w[0][j + 1];
+        w[1][j] = (__bf16)r0;
+        w[1][j + 1] = (__bf16)r1;
+        w[2][j] = (__bf16)(r0 - (float)w[1][j]);
+        w[2][j + 1] = (__bf16)(r1 - (float)w[1][j + 1]);
+    }
 }
 
 // Which of a lane's eight consecutive values of a dim belong to a token in front of `count`: the others are whatever the memory
@@ -108,5 +112,36 @@ __device__ inline void store4(void* o, int64_t at, int d, int D, const float (&x
             for (int i = 0; i < 3; ++i) if (d + i < D) p[i] = u[i];
     }
 }
+
+// ---- parts ------------------------------------------------------------------------------------------------------------------------
+// Where few rows meet long sequences, several workgroups share a row's keys.  Each leaves its sums over the values and its m and l (all
+// 32 bits) in the workspace, split s of row `row` (row of q times heads, plus head) at place row * splits + s, and a second launch joins them:
+//   m = max m_s,  o = sum_s exp(m_s - m) sums_s / sum_s exp(m_s - m) l_s.
+struct Parts {
+    float* sums;                       // [rows][splits][D]
+    float* state;                      // [rows][splits][2]: m, l
+    int splits, least;                 // workgroups for a row, and blocks (of 32 tokens, or stages of 64) that one has at least
+    Parts() : sums(nullptr), state(nullptr), splits(1), least(1) {}
+    Parts(void* workspace, int64_t rows, int splits_, int least_, int D)
+        : sums(static_cast<float*>(workspace)), state(sums + rows * splits_ * D), splits(splits_), least(least_) {}
+    static size_t bytes(int64_t rows, int splits, int D) { return splits < 2 ? 0 : ((size_t)(rows * splits) * (D + 2) * 4 + 15) / 16 * 16; }
+    __device__ int run(int units) const { const int n = (units + splits - 1) / splits; return n < least ? least : n; }
+};
+constexpr int kMostSplits = 256;       // of a row: one to a thread of the join
+
+// Joins the splits of each row; `rows_a_tile` 0: rows of single tokens, dealt out by blocks; otherwise the prefill kernel's tile.
+struct JoinArgs {
+    void* o;
+    float scale;                       // of the softmax, times log2 e
+    int heads, group, T, rows_a_tile;
+};
+hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream);
+
+// The prefill kernel's tile of a sequence's rows for one head: the keys that its last token sees, in stages of 64 tokens.
+constexpr int kStageTokens = 64;
+__device__ inline int tile_sees(const NewTokens& nt, int64_t row_last, int group) { return nt.pos0 + (int)(row_last / group) + 1; }
+__device__ inline int stages_of(int seen) { return seen > 0 ? (seen + kStageTokens - 1) / kStageTokens : 0; }
+
+__device__ inline int blocks_of(const KvView& kv, int b) { return (kv.length(kv.kv_len[b]) + kKvBlock - 1) / kKvBlock; }
 
 }  // namespace bitnet

@@ -15,36 +15,43 @@ namespace {
 struct DecodeArgs {
     const uint16_t* q;
     void* o;
-    float* part;                       // partial sums, or NULL
     float scale;                       // of the softmax, times log2 e
     int heads, group;                  // query heads, and of them per key-value head
     int column_tiles;                  // of 16 query heads, per key-value head
 };
 
+// A row is 16 query heads (or what a group has left) of one key-value head of one sequence.  Its blocks are dealt out to up to
+// parts.splits workgroups (blockIdx.y).
 template <int kC, bool kExact, bool kF32, int kW>
-__global__ __launch_bounds__(64 * kW) void attention_decode_rows(DecodeArgs a, KvView kv) {
+__global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_rows(DecodeArgs a, Parts parts, KvView kv) {
     constexpr int kV = 2 * kC;                             // tiles of 16 dims
-    constexpr int kRound = kV < 4 ? kV : 4;                // ... that the waves add up at a time
+    constexpr int kWholeChunks = whole_chunks(kC);
+    constexpr int kRound = kV < 4 ? kV : 4;                // tiles that the waves add up at a time
     constexpr int kPitch = 16 * kRound + 4;
     __shared__ float sums[kW * 16 * kPitch], maxima[kW * 16], totals[kW * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int D = kExact ? 32 * kC : kv.D, Dp = kv_padded_dim(D), quads = Dp >> 3;
-    int row = blockIdx.x;
-    const int ct = row % a.column_tiles;
-    row /= a.column_tiles;
-    const int h = row % kv.kv_heads, b = row / kv.kv_heads;
+    const int rows_a_sequence = kv.kv_heads * a.column_tiles, b = blockIdx.x / rows_a_sequence, rest = blockIdx.x - b * rows_a_sequence;
+    const int h = rest / a.column_tiles, ct = rest - h * a.column_tiles;
     const int head0 = h * a.group + 16 * ct, columns = min(a.group - 16 * ct, 16);
+    // What does not hang on the sequence's length is requested along with it: the queries, and of the page table the first 64
+    // entries, one a lane, which are all of it more often than not.
+    const int32_t* table = kv.table + b * kv.table_stride;
+    const bool short_table = kv.max_pages <= 64;
+    const int pages = short_table && lane < kv.max_pages ? table[lane] : -1;
     const int len = kv.length(kv.kv_len[b]), blocks = (len + kKvBlock - 1) / kKvBlock;
+    const int run = parts.run(blocks), blk0 = blockIdx.y * run, blk1 = min(blk0 + run, blocks);
+    if (blk0 >= blocks && blockIdx.y > 0) return;
 
     v8bf qf[kC];
     load_query<kC>(qf, r < columns ? a.q + ((int64_t)b * a.heads + head0 + r) * D : nullptr, g, D);
 
     int koff[kC], voff[kV];                                // bytes within a block
 #pragma unroll
-    for (int c = 0; c < kC; ++c) koff[c] = (kExact ? 4 * c + g : min(4 * c + g, quads - 1)) * 512 + r * 16;
+    for (int c = 0; c < kC; ++c) koff[c] = (kExact || c < kWholeChunks ? 4 * c + g : min(4 * c + g, quads - 1)) * 512 + r * 16;
 #pragma unroll
-    for (int i = 0; i < kV; ++i) voff[i] = (g * Dp + (kExact ? 16 * i + r : min(16 * i + r, Dp - 1))) * 16;
+    for (int i = 0; i < kV; ++i) voff[i] = (g * Dp + (kExact || i < 2 * kWholeChunks ? 16 * i + r : min(16 * i + r, Dp - 1))) * 16;
 
     v4f acc[kV];
 #pragma unroll
@@ -52,13 +59,14 @@ __global__ __launch_bounds__(64 * kW) void attention_decode_rows(DecodeArgs a, K
     float m = kMinusInf, l = 0.0f;                         // l: of this lane's tokens
 
     struct Block { v4u k[kC][2], v[kV]; };
-    // this wave's blocks are wave, wave + kW, ...; their numbers in the cache stand in the lanes, 64 at a time
-    const int mine = blocks > wave ? (blocks - wave + kW - 1) / kW : 0;
-    const int32_t* table = kv.table + b * kv.table_stride;
+    // this wave's blocks are first, first + kW, ...; their numbers in the cache stand in the lanes, 64 at a time
+    const int first = blk0 + wave, mine = blk1 > first ? (blk1 - first + kW - 1) / kW : 0;
     int numbers = -1;
     auto fetch_numbers = [&](int it) {
-        const int blk = wave + (it + lane) * kW;
-        numbers = blk < blocks ? kv.block(table, blk, h) : -1;
+        const int blk = first + (it + lane) * kW, p = blk / kv.page_blocks;
+        int page = short_table ? __shfl(pages, p) : -1;
+        if (!short_table && blk < blk1) page = table[p];
+        numbers = blk < blk1 ? kv.block_on(page, blk - p * kv.page_blocks, h) : -1;
     };
     const int64_t block_bytes = (int64_t)kKvBlock * Dp * 2;
     auto load = [&](Block& x, int it) {
@@ -72,7 +80,7 @@ __global__ __launch_bounds__(64 * kW) void attention_decode_rows(DecodeArgs a, K
         for (int i = 0; i < kV; ++i) x.v[i] = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(v + voff[i]));
     };
     auto take = [&](Block& x, int it, bool known /* whether the block's page exists */) {
-        const int left = known ? len - kKvBlock * (wave + it * kW) : 0;      // of the block's tokens, how many count
+        const int left = known ? len - kKvBlock * (first + it * kW) : 0;      // of the block's tokens, how many count
         v4f s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
         for (int c = 0; c < kC; ++c)
@@ -102,14 +110,13 @@ __global__ __launch_bounds__(64 * kW) void attention_decode_rows(DecodeArgs a, K
             p[j] = exp2_fast(__builtin_fmaf(p[j], a.scale, -base));
             l += p[j];
         }
-        const v8bf w = weights_operand(p);
+        v8bf w[kF32 ? 3 : 1];
 #pragma unroll
-        for (int i = 0; i < kV; ++i) acc[i] = mfma_bf16(__builtin_bit_cast(v8bf, x.v[i]), w, acc[i]);
-        if (kF32) {
-            const v8bf rest = weights_rest(p, w);
+        for (int j = 0; j < 8; j += 2) weights_pair<kF32>(w, j, p[j], p[j + 1]);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) acc[i] = mfma_bf16(__builtin_bit_cast(v8bf, x.v[i]), rest, acc[i]);
-        }
+        for (int e = 0; e < (kF32 ? 3 : 1); ++e)
+#pragma unroll
+            for (int i = 0; i < kV; ++i) acc[i] = mfma_bf16(__builtin_bit_cast(v8bf, x.v[i]), w[e], acc[i]);
     };
     Block x0, x1;
     if (mine > 0) {
@@ -153,53 +160,90 @@ __global__ __launch_bounds__(64 * kW) void attention_decode_rows(DecodeArgs a, K
             }
         __syncthreads();
         for (int i = threadIdx.x; i < columns * 4 * kRound; i += 64 * kW) {
-            const int col = i / (4 * kRound), d = (i % (4 * kRound)) * 4;
+            const int col = i / (4 * kRound), d = (i % (4 * kRound)) * 4, dim = 16 * kRound * round + d;
+            if (dim >= D) continue;
             float top = kMinusInf, total = 0.0f;
 #pragma unroll
             for (int w = 0; w < kW; ++w) top = fmaxf(top, maxima[w * 16 + col]);
             v4f x = {0, 0, 0, 0};
 #pragma unroll
             for (int w = 0; w < kW; ++w) {
+                const float mw = maxima[w * 16 + col];
                 x += *reinterpret_cast<const v4f*>(&sums[(w * 16 + col) * kPitch + d]);
-                total += maxima[w * 16 + col] == kMinusInf ? 0.0f : totals[w * 16 + col] * exp2_fast((maxima[w * 16 + col] - top) * a.scale);
+                total += mw == kMinusInf ? 0.0f : totals[w * 16 + col] * exp2_fast((mw - top) * a.scale);
             }
-            const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-            const float out[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
-            const int dim = 16 * kRound * round + d;
-            if (dim < D) store4<kF32>(a.o, ((int64_t)b * a.heads + head0 + col) * D, dim, D, out);
+            if (run >= blocks) {
+                const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+                const float out[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+                store4<kF32>(a.o, ((int64_t)b * a.heads + head0 + col) * D, dim, D, out);
+            } else {
+                const float out[4] = {x[0], x[1], x[2], x[3]};
+                const int64_t place = ((int64_t)b * a.heads + head0 + col) * parts.splits + blockIdx.y;
+                store4<true>(parts.sums, place * D, dim, D, out);
+                if (dim == 0) {
+                    parts.state[2 * place] = top;
+                    parts.state[2 * place + 1] = total;
+                }
+            }
         }
         __syncthreads();
     }
 }
 
 template <int kC, bool kExact>
-hipError_t launch_rows(const DecodeArgs& a, const KvView& kv, bool f32, hipStream_t stream) {
-    const int64_t rows = (int64_t)kv.B * kv.kv_heads * a.column_tiles;
-    if (f32) attention_decode_rows<kC, kExact, true, 4><<<(unsigned)rows, 256, 0, stream>>>(a, kv);
-    else attention_decode_rows<kC, kExact, false, 4><<<(unsigned)rows, 256, 0, stream>>>(a, kv);
-    return hipGetLastError();
+hipError_t launch_decode(const DecodeArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream) {
+    const dim3 grid((unsigned)((int64_t)kv.B * kv.kv_heads * a.column_tiles), parts.splits);
+    if (f32) attention_decode_rows<kC, kExact, true, 4><<<grid, 256, 0, stream>>>(a, parts, kv);
+    else attention_decode_rows<kC, kExact, false, 4><<<grid, 256, 0, stream>>>(a, parts, kv);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || parts.splits < 2) return e;
+    return launch_attention_join({a.o, a.scale, a.heads, a.group, kv.B, 0}, parts, kv, f32, stream);
+}
+
+// How many workgroups share a row at most, by the length that the page tables have room for.  A CU draws 25 to 45 bytes a cycle,
+// whatever number of waves asks, and a second launch costs 4 us in a chain of launches: so rows are shared where there are fewer
+// than 256 and more than 1023 tokens (one token, 32 heads of 128, a key-value head each, 1000 tokens: 13.4 us in one launch, 10.0 shared;
+// 500 tokens 8.6 / 9.4; 64 heads over 8, 1000 tokens 9.4 / 9.4), until there are two for each CU (three sequences of 23000 to 41000
+// tokens, 64 heads over 8: 512 workgroups 74.7 us, 1024 79.1, 2048 79.2, none shared 359).  More rows are shared only at every
+// 8192 tokens, so that one long sequence among short ones is not what the call waits for.
+struct Splits { int n, least; };
+Splits decode_splits(const KvView& kv, int heads) {
+    const int64_t rows = (int64_t)kv.B * kv.kv_heads * ceil_div(heads / kv.kv_heads, 16);
+    constexpr int kShort = 8, kLong = 256;                 // blocks: two for each wave of a workgroup; 8192 tokens
+    if (kv.max_blocks < 32) return {1, 1};
+    const int64_t fill = rows < 256 ? 512 / rows : 1, long_ones = ceil_div(kv.max_blocks, kLong), room = 8192 / rows;
+    const int least = fill > 1 ? kShort : kLong / 2;
+    int64_t n = fill > long_ones ? fill : long_ones < room ? long_ones : room;
+    const int64_t most = ceil_div(kv.max_blocks, least);
+    n = n < most ? n : most;
+    return {(int)(n < 1 ? 1 : n > kMostSplits ? kMostSplits : n), least};
 }
 
 }  // namespace
 
-size_t attention_decode_workspace_bytes(const KvView&, int) { return 0; }
+size_t attention_decode_workspace_bytes(const KvView& kv, int heads) {
+    return Parts::bytes((int64_t)kv.B * heads, decode_splits(kv, heads).n, kv.D);
+}
 
 hipError_t launch_attention_decode(const void* q, const KvView& kv, int heads, float scale, void* o, bool f32, void* workspace,
                                    size_t workspace_bytes, hipStream_t stream) {
-    DecodeArgs a{static_cast<const uint16_t*>(q), o, nullptr, scale * 1.44269504f, heads, heads / kv.kv_heads, 0};
-    a.column_tiles = (int)ceil_div(a.group, 16);
+    const int group = heads / kv.kv_heads;
+    const DecodeArgs a{static_cast<const uint16_t*>(q), o, scale * 1.44269504f, heads, group, (int)ceil_div(group, 16)};
+    Parts parts;
+    const Splits s = decode_splits(kv, heads);
+    if (s.n > 1 && workspace_bytes >= attention_decode_workspace_bytes(kv, heads)) parts = Parts(workspace, (int64_t)kv.B * heads, s.n, s.least, kv.D);
     const int chunks = (int)ceil_div(kv.D, 32);
     const bool exact = kv.D % 32 == 0;
-#define ROWS(kC_) return exact ? launch_rows<kC_, true>(a, kv, f32, stream) : launch_rows<kC_, false>(a, kv, f32, stream)
+#define DECODE(kC_) return exact && chunks == kC_ ? launch_decode<kC_, true>(a, parts, kv, f32, stream) : launch_decode<kC_, false>(a, parts, kv, f32, stream)
     switch (chunks) {
-        case 1: ROWS(1);
-        case 2: ROWS(2);
-        case 3: ROWS(3);
-        case 4: ROWS(4);
-        case 5: case 6: return chunks == 6 && exact ? launch_rows<6, true>(a, kv, f32, stream) : launch_rows<6, false>(a, kv, f32, stream);
-        default: return chunks == 8 && exact ? launch_rows<8, true>(a, kv, f32, stream) : launch_rows<8, false>(a, kv, f32, stream);
+        case 1: DECODE(1);
+        case 2: DECODE(2);
+        case 3: DECODE(3);
+        case 4: DECODE(4);
+        case 5: case 6: DECODE(6);
+        default: DECODE(8);
     }
-#undef ROWS
+#undef DECODE
 }
 
 }  // namespace bitnet

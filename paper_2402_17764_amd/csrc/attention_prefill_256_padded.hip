@@ -1,0 +1,6 @@
+// The prefill attention kernels for heads of 194 to 254 dims.
+#include "attention_prefill_kernel.hpp"
+
+namespace bitnet {
+template hipError_t launch_prefill<8, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
+}

@@ -1,0 +1,343 @@
+// Attention of runs of new tokens over their sequences' caches, causal: the token at position p sees the keys of positions 0 ... p.
+//   s_j = scale q . k_j (j <= p),  p = softmax(s),  o = sum_j p_j v_j,
+// with the running maximum and sum of a softmax in 32 bits, one pass over the keys.
+//
+// A workgroup takes a tile of rows of one sequence and one key-value head -- a row is one query head of one new token, the heads of a
+// group next to each other, so that grouped heads share what they read -- and walks the cache 64 tokens at a time.  Both cache
+// blocks come through LDS (copied as they stand, by loads that go to LDS directly; the cache's order is already that of the MFMA
+// operands), double-buffered: the next blocks are requested right behind the barrier that publishes the current ones.  Scores are products
+// keys (down) times queries (across), which leaves a lane with eight consecutive tokens of its query: the operand of the second product.
+#pragma once
+#include "attention_common.hpp"
+
+#include <type_traits>
+
+namespace bitnet {
+
+struct PrefillArgs {
+    const uint16_t* q;
+    void* o;
+    float scale;                       // of the softmax, times log2 e
+    int heads, group, T;               // query heads, and of them per key-value head; rows of q
+    int tiles;                         // of the launch, per key-value head
+};
+
+// The shapes of a workgroup: four waves of one or two times 16 rows each (heads of more than 128 dims: four or eight waves of 16, as a wave's
+// sums take its registers), and stages of LDS of one cache block, or two where a block is small.  Both leave room for three or
+// four workgroups on a CU, which is what hides a stage's barrier and the chain of loads that a workgroup begins with (us, one prompt of
+// 2048 tokens and 40 heads of 128 / sixteen of 100 to 400 and 64 heads over 8 / one of 1024 behind 15000, 64 over 8: 64 rows and
+// one block 60 / 58 / 539, two blocks 66 / 80 / 579; 128 rows and one block 61 / 54 / 466, two blocks 58 / 66 / 466; 256 rows in
+// eight waves, two blocks 67 / 74 / 456; 256 rows in four waves, whose sums move to and from the accumulation registers, 100 / - / 591).
+enum class PrefillTile { Rows64, Rows128 };
+constexpr int prefill_rows(PrefillTile t) { return t == PrefillTile::Rows64 ? 64 : 128; }
+constexpr float kSlack = 8.0f;         // in the exponent of 2
+
+constexpr int prefill_piece(int Dp) { return (Dp * 64 + 1023) / 1024 * 1024; }     // a block's keys (or values) in LDS: whole wave loads
+
+template <int kC, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
+__global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(PrefillArgs a, Parts parts, KvView kv) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kV = 2 * kC, kRows = 16 * kNT * kW, kU = kStageBlocks;   // cache blocks of a stage
+    constexpr int kPerUnit = kStageTokens / (kKvBlock * kStageBlocks);
+    extern __shared__ uint4 smem[];
+    __shared__ int bad_at[256 + 4];                                        // of each dim: the first position whose value is not finite
+    for (int i = threadIdx.x; i < 256 + 4; i += 64 * kW) bad_at[i] = 0x7FFFFFFF;
+    char* lds = reinterpret_cast<char*>(smem);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int D = kExact ? 32 * kC : kv.D, Dp = kv_padded_dim(D), quads = Dp >> 3;
+    const int piece = kExact ? prefill_piece(32 * kC) : prefill_piece(Dp), stage_bytes = 2 * kStageBlocks * piece;
+
+    // Heads side by side: with a multiple of eight of them a head's tiles meet on one XCD, whose L2 then holds its keys and values once.
+    const int h = blockIdx.x % kv.kv_heads;
+    const int64_t x = a.tiles - 1 - (int)(blockIdx.x / kv.kv_heads);       // late tiles, which see most, first
+    const int b = sequence_of_tile(kv.q_start, kv.B, x, a.group, kRows, 1);
+    const NewTokens nt(kv, b, a.T);
+    const int64_t tile = x - first_tile(kv.q_start[b], b, a.group, kRows, 1);
+    const int64_t rows = (int64_t)nt.n * a.group;
+    if (tile < 0 || tile * kRows >= rows) return;
+    const int64_t row0 = tile * kRows;                                     // of the sequence's rows for this head
+    const int64_t row_last = min(row0 + kRows, rows) - 1;
+    const int seen = tile_sees(nt, row_last, a.group);                     // keys that the tile's last token sees
+    const int blocks = seen > 0 ? (seen + kKvBlock - 1) / kKvBlock : 0, all_stages = stages_of(seen);
+    // this workgroup's stages
+    const int run = parts.run(all_stages), stage0 = blockIdx.y * run * kPerUnit;
+    const int stages = min(stage0 + run * kPerUnit, (blocks + kStageBlocks - 1) / kStageBlocks);
+    if (blockIdx.y > 0 && stage0 >= stages) return;
+
+    v8bf qf[kNT][kC];
+    int pos[kNT];                                                          // of the lane's queries; -1: none
+    int out_row[kNT];                                                      // row of q times heads, plus head; -1: none
+    const int64_t wave_row = row0 + wave * 16 * kNT;
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+        const int64_t R = wave_row + 16 * n + r;
+        const int tok = (int)(R / a.group), hh = (int)(R - (int64_t)tok * a.group);
+        out_row[n] = R < rows ? (nt.first + tok) * a.heads + h * a.group + hh : -1;
+        pos[n] = R < rows ? nt.pos0 + tok : -1;
+        load_query<kC>(qf[n], R < rows ? a.q + (int64_t)out_row[n] * D : nullptr, g, D);
+    }
+    const int tile_pos = nt.pos0 + (int)(row0 / a.group);                  // of the tile's first token, and of the wave's last
+    const int pos_last = wave_row < rows ? nt.pos0 + (int)((min(wave_row + 16 * kNT, rows) - 1) / a.group) : -1;
+
+    const int32_t* table = kv.table + b * kv.table_stride;
+    int numbers = -1;                                                      // of 64 blocks, one a lane
+    auto fetch_numbers = [&](int blk0) {
+        const int blk = blk0 + lane;
+        numbers = blk < blocks ? kv.block(table, blk, h) : -1;
+    };
+    const int64_t block_bytes = (int64_t)kKvBlock * Dp * 2;
+    // 1 KiB at a time: the stage's key blocks, then its value blocks, dealt out to the waves.  What a block's padding to whole loads reaches
+    // behind the block's end comes back as zeros.
+    auto copy = [&](int stage) {
+        constexpr int kLoads = 2 * kC, kAll = 2 * kStageBlocks * kLoads;
+        char* to = lds + (stage & 1) * stage_bytes;
+#pragma unroll
+        for (int j = 0; j < (kAll + kW - 1) / kW; ++j) {
+            const int p = j * kW + wave;
+            if (kAll % kW && p >= kAll) break;
+            const int what = kLoads % kW == 0 ? j * kW / kLoads : p / kLoads, i = kLoads % kW == 0 ? j * kW % kLoads + wave : p % kLoads;
+            if (!kExact && i >= piece >> 10) continue;
+            const int64_t at = max(__builtin_amdgcn_readlane(numbers, (stage * kStageBlocks + what % kStageBlocks) & 63), 0) * block_bytes;
+            const __amdgpu_buffer_rsrc_t rsrc =
+                __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(what < kStageBlocks ? kv.k : kv.v) + at, 0, (int)block_bytes, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + what * piece + i * 1024), 16, i * 1024 + lane * 16, 0, 0, 0);
+        }
+    };
+    int koff[kC], voff[kV];
+#pragma unroll
+    for (int c = 0; c < kC; ++c) koff[c] = (kExact || c < whole_chunks(kC) ? 4 * c + g : min(4 * c + g, quads - 1)) * 512 + r * 16;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) voff[i] = (g * Dp + (kExact || i < 2 * whole_chunks(kC) ? 16 * i + r : min(16 * i + r, Dp - 1))) * 16;
+
+    v4f acc[kNT][kV];
+    float m[kNT], l[kNT];
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+        m[n] = kMinusInf;
+        l[n] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) acc[n][i] = (v4f){0, 0, 0, 0};
+    }
+    // A stage's blocks, in LDS from `keys` and `values` on, the first token at position j0.  Masked: some row does not see all of them.
+    //
+    // A wave's matrix instructions run beside its exponentials where the source puts them so, a slice at a time with a fence behind each: the
+    // scores of the second block with the weights of the first, the values of the first with the weights of the second.  Operands are read
+    // from LDS kAhead fragments ahead of their products, keys and values in one sequence.
+    constexpr int kParts = kF32 ? 3 : 1, kAhead = 4, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
+    auto take = [&](auto masked_, const char* keys, const char* values, int j0, const bool (&known)[kU]) {
+        constexpr bool kMasked = decltype(masked_)::value;
+        v4f sc[kU][2][kNT];
+        v8bf w[kU][kNT][kParts], frag[kAhead];
+        float base[kNT];
+        auto read = [&](int f) {
+            if (f < kKeys * kU) frag[f % kAhead] = *reinterpret_cast<const v8bf*>(keys + f / kKeys * piece + koff[f / 2 % kC] + 256 * (f & 1));
+            else if (f < (kKeys + kV) * kU)
+                frag[f % kAhead] = *reinterpret_cast<const v8bf*>(values + (f - kKeys * kU) / kV * piece + voff[(f - kKeys * kU) % kV]);
+        };
+        // the i-th of `slices` shares of block u's weights, two at a time
+        auto weights = [&](int u, int i, int slices) {
+#pragma unroll
+            for (int q = i * (4 * kNT) / slices; q < (i + 1) * (4 * kNT) / slices; ++q) {
+                const int n = q / 4, j = q % 4 * 2;
+                const float p0 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][j & 3], a.scale, -base[n]));
+                const float p1 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][(j & 3) + 1], a.scale, -base[n]));
+                l[n] += p0;
+                l[n] += p1;
+                weights_pair<kF32>(w[u][n], j, p0, p1);
+            }
+        };
+        auto scores = [&](int u, int with) {
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) {
+                const int f = u * kKeys + i, c = i / 2, t = i & 1;
+#pragma unroll
+                for (int n = 0; n < kNT; ++n) sc[u][t][n] = mfma_bf16(frag[f % kAhead], qf[n][c], c ? sc[u][t][n] : (v4f){0, 0, 0, 0});
+                read(f + kAhead);
+                if (with >= 0) weights(with, i, kKeys);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto product = [&](int u, int with) {
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                const int f = kU * kKeys + u * kV + i;
+#pragma unroll
+                for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                    for (int e = 0; e < kParts; ++e) acc[n][i] = mfma_bf16(frag[f % kAhead], w[u][n][e], acc[n][i]);
+                read(f + kAhead);
+                if (with >= 0) weights(with, i, kV);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        // The maximum so far against block u's scores.  One that is passed by less than kSlack stays: weights up to 2^kSlack lose nothing in
+        // 32-bit sums nor, being floating-point numbers, in bf16.  Otherwise what has been summed is rescaled, together with the values of
+        // the block in front of u, whose weights went by the old maximum.
+        auto check = [&](int u) {
+            bool passed = false;
+            float tops[kNT];
+#pragma unroll
+            for (int n = 0; n < kNT; ++n) {
+                if (kMasked)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (!known[u] || j0 + u * kKvBlock + 8 * g + j > pos[n]) sc[u][j >> 2][n][j & 3] = kMinusInf;
+                float top = sc[u][0][n][0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[u][j >> 2][n][j & 3]);
+                tops[n] = top;
+                passed = passed || top * a.scale > m[n] * a.scale + kSlack;
+            }
+            if (__builtin_amdgcn_ballot_w64(passed)) {
+                if (u > 0) {
+#pragma unroll
+                    for (int i = 0; i < kV; ++i) {
+                        const v8bf v = *reinterpret_cast<const v8bf*>(values + (u - 1) * piece + voff[i]);
+#pragma unroll
+                        for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                            for (int e = 0; e < kParts; ++e) acc[n][i] = mfma_bf16(v, w[u - 1][n][e], acc[n][i]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < kNT; ++n) {
+                    const float now = fmaxf(m[n], groups_max(tops[n])), by = now == kMinusInf ? 1.0f : exp2_fast((m[n] - now) * a.scale);
+                    m[n] = now;
+                    l[n] *= by;
+#pragma unroll
+                    for (int i = 0; i < kV; ++i) acc[n][i] *= by;
+                    if (u > 0)
+#pragma unroll
+                        for (int e = 0; e < kParts; ++e) w[u - 1][n][e] = v8bf{};
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < kNT; ++n) base[n] = m[n] == kMinusInf ? 0.0f : m[n] * a.scale;
+            __builtin_amdgcn_sched_barrier(0);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read(i);
+        scores(0, -1);
+        check(0);
+        if (kU == 2) {
+            scores(kU - 1, 0);
+            check(kU - 1);
+            product(0, kU - 1);
+        } else {
+            weights(0, 0, 1);
+        }
+        product(kU - 1, -1);
+    };
+    auto stage_there = [&](int s) {                                        // publishes stage s, requests the next
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (s + 1 < stages) {
+            if ((((s + 1) * kStageBlocks) & 63) == 0) fetch_numbers((s + 1) * kStageBlocks);
+            copy(s + 1);
+        }
+    };
+    __syncthreads();
+    if (stage0 < stages) {
+        fetch_numbers((stage0 * kStageBlocks) & ~63);
+        copy(stage0);
+    }
+    // The values of a stage that some row does not see to its end.  A weight of zero does not make an infinity nothing: tokens that no row sees
+    // are cleared in LDS, and of the others what is not finite, which is noted: rows that see it get NaN in its dim at the end, the rows in
+    // front of it their sums.
+    auto clean = [&](char* values, int j0, const bool (&known)[kStageBlocks]) {
+        for (int i = threadIdx.x; i < kStageBlocks * 4 * Dp; i += 64 * kW) {
+            const int u = i / (4 * Dp), at = i - u * 4 * Dp, first = j0 + u * kKvBlock + at / Dp * 8, d = at % Dp;
+            const int some = known[u] ? min(max(seen - first, 0), 8) : 0;
+            uint4* place = reinterpret_cast<uint4*>(values + u * piece + at * 16);
+            v4u v = __builtin_bit_cast(v4u, *place);
+            values_keep(v, some);
+            unsigned bad = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= (unsigned)((v[e] & 0x7F80u) == 0x7F80u) | (unsigned)((v[e] & 0x7F800000u) == 0x7F800000u);
+            if (bad) {
+                for (int e = 7; e >= 0; --e) {
+                    const unsigned half = 0xFFFFu << (16 * (e & 1)), exponent = 0x7F80u << (16 * (e & 1));
+                    if ((v[e >> 1] & exponent) != exponent) continue;
+                    v[e >> 1] &= ~half;
+                    atomicMin(&bad_at[d], first + e);
+                }
+            }
+            if (bad || some < 8) *place = __builtin_bit_cast(uint4, v);
+        }
+    };
+    int s = stage0;
+    // Stages that all rows of the tile see, and all of whose pages exist; then the others.
+    for (; s < stages; ++s) {
+        const int j0 = s * kStageBlocks * kKvBlock, at = (s * kStageBlocks) & 63;
+        if (j0 + kStageBlocks * kKvBlock - 1 > tile_pos || __builtin_amdgcn_readlane(numbers, at) < 0 || __builtin_amdgcn_readlane(numbers, at + kStageBlocks - 1) < 0) break;
+        stage_there(s);
+        const char* keys = lds + (s & 1) * stage_bytes;
+        const char* values = keys + kStageBlocks * piece;
+        const bool known[kU] = {};
+        take(std::false_type(), keys, values, j0, known);
+    }
+    for (; s < stages; ++s) {
+        const int j0 = s * kStageBlocks * kKvBlock;
+        bool known[kStageBlocks];
+#pragma unroll
+        for (int u = 0; u < kStageBlocks; ++u) known[u] = __builtin_amdgcn_readlane(numbers, (s * kStageBlocks + u) & 63) >= 0;
+        stage_there(s);
+        char* keys = lds + (s & 1) * stage_bytes;
+        char* values = keys + kStageBlocks * piece;
+        clean(values, j0, known);
+        __syncthreads();
+        if (j0 > pos_last) continue;                                       // nothing that this wave's rows see
+        take(std::true_type(), keys, values, j0, known);
+    }
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+        const float total = groups_sum(l[n]), inv = total > 0.0f ? 1.0f / total : 0.0f;
+        if (out_row[n] < 0) continue;
+        const int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
+        const bool whole = run >= all_stages;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int d = 16 * i + 4 * g;
+            if (d >= D) continue;
+            float out[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = pos[n] >= bad_at[d + e] ? __builtin_nanf("") : whole ? acc[n][i][e] * inv : acc[n][i][e];
+            if (whole) store4<kF32>(a.o, (int64_t)out_row[n] * D, d, D, out);
+            else store4<true>(parts.sums, place * D, d, D, out);
+        }
+        if (!whole && g == 0) {
+            parts.state[2 * place] = m[n];
+            parts.state[2 * place + 1] = total;
+        }
+    }
+#endif
+}
+
+template <int kC, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
+hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView& kv, hipStream_t stream) {
+    static RaisedFlags raised;
+    const auto kernel = attention_prefill_tiles<kC, kExact, kNT, kStageBlocks, kW, kOcc, kF32>;
+    const int lds = 2 * 2 * kStageBlocks * prefill_piece(kv_padded_dim(kv.D));
+    if (lds > 65536 - 2048) {                              // with the static part
+        const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(kernel), 2 * 2 * kStageBlocks * prefill_piece(32 * kC), raised);
+        if (e != hipSuccess) return e;
+    }
+    a.tiles = (int)tiles_at_most(a.T, kv.B, a.group, 16 * kNT * kW, 1);
+    kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, lds, stream>>>(a, parts, kv);
+    return hipGetLastError();
+}
+template <int kC, bool kExact, bool kF32>
+hipError_t launch_prefill_form(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, hipStream_t stream) {
+    constexpr int kStageBlocks = kC <= 2 ? 2 : 1;
+    if (tile == PrefillTile::Rows64) return launch_prefill_tiles<kC, kExact, 1, kStageBlocks, 4, kC <= 4 ? 4 : 2, kF32>(a, parts, kv, stream);
+    return launch_prefill_tiles<kC, kExact, kC <= 4 ? 2 : 1, kStageBlocks, kC <= 4 ? 4 : 8, kC <= 4 && !kF32 ? 3 : 2, kF32>(a, parts, kv, stream);
+}
+// compiled in translation units of their own
+template <int kC, bool kExact>
+hipError_t launch_prefill(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream) {
+    return f32 ? launch_prefill_form<kC, kExact, true>(tile, a, parts, kv, stream) : launch_prefill_form<kC, kExact, false>(tile, a, parts, kv, stream);
+}
+
+}  // namespace bitnet

@@ -30,17 +30,21 @@ struct KvView {
     uint16_t *k, *v;
     const int32_t *table, *kv_len, *q_start;
     int64_t table_stride;
-    int32_t pages, page_blocks, max_blocks /* a table row's: pages times page_blocks */, kv_heads, D, B;
+    int32_t pages, page_blocks /* of a page, for one head */, max_pages /* of a table row */, max_blocks /* ... times page_blocks */, kv_heads, D, B;
 
     // tokens of sequence b that can be in the cache
     BITNET_BOTH int length(int32_t len) const {
         const int64_t most = (int64_t)max_blocks * kKvBlock;
         return len < 0 ? 0 : len > most ? (int)most : len;
     }
-    // block `blk` of a sequence, 0 <= blk < max_blocks, for key-value head h: its number in the cache, or -1 where the table names no page
+    // block `in` of a page, as the table names it, for key-value head h: its number in the cache, or -1 where there is no such page
+    BITNET_BOTH int block_on(int page, int in, int h) const {
+        return page < 0 || page >= pages ? -1 : (page * kv_heads + h) * page_blocks + in;
+    }
+    // the same for block `blk` of a sequence, 0 <= blk < max_blocks
     BITNET_BOTH int block(const int32_t* row, int blk, int h) const {
-        const int p = blk / page_blocks, page = row[p];
-        return page < 0 || page >= pages ? -1 : (page * kv_heads + h) * page_blocks + (blk - p * page_blocks);
+        const int p = blk / page_blocks;
+        return block_on(row[p], blk - p * page_blocks, h);
     }
 };
 
@@ -72,6 +76,8 @@ BITNET_BOTH inline int sequence_of_tile(const int32_t* q_start, int B, int64_t x
     }
     return lo;
 }
-BITNET_BOTH inline int64_t tiles_at_most(int64_t T, int64_t B, int each, int size, int extra) { return T * each / size + extra * B; }
+BITNET_BOTH inline int64_t tiles_at_most(int64_t T, int64_t B, int each, int size, int extra) {
+    return extra == 1 ? (T * each + size - 1) / size + B - 1 : T * each / size + extra * B;
+}
 
 }  // namespace bitnet

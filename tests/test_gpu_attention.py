@@ -247,6 +247,20 @@ def test_prefill_lengths(gpu_lib, sizes, heads, kv_heads, D):
     run_prefill(gpu_lib, sizes, heads, kv_heads, D, 64, len(sizes) == 1, seed=2, rows=40)
 
 
+# tiles of 128 rows: a long prompt, and a chunk behind a long context, whose last tiles are filled in part
+@pytest.mark.parametrize("D", [64, 100, 128, 192])
+@pytest.mark.parametrize("sizes", [[(0, 2100)], [(4500, 1030)], [(0, 1500), (7, 777)]])
+def test_prefill_long_runs(gpu_lib, D, sizes):
+    run_prefill(gpu_lib, sizes, 64, 8, D, 64, len(sizes) == 1, seed=4, rows=24)
+
+
+# rows that several workgroups share, of sequences some of which are too short for that, or end where a share begins
+@pytest.mark.parametrize("D", [64, 100, 128, 256])
+@pytest.mark.parametrize("sizes", [[(3000, 5)], [(2000, 20), (0, 3), (255, 1), (256, 1)], [(1500, 0), (1040, 70)], [(-2, 4), (1100, 2)]])
+def test_prefill_shared_rows(gpu_lib, D, sizes):
+    run_prefill(gpu_lib, sizes, 6, 2, D, 32, D != 128, seed=5, first=1, behind=2)
+
+
 def test_prefill_values_that_are_not_finite_stay_with_the_rows_that_see_them(gpu_lib):
     heads, kv_heads, D, P = 4, 2, 64, 32
     for n, at, value in [(100, 40, np.inf), (100, 99, np.nan), (300, 64, -np.inf), (70, 0, np.nan)]:

@@ -16,7 +16,7 @@ using namespace bitnet;
 extern "C" int key_at(int t, int d) { return kv_key_at(t, d); }
 extern "C" int value_at(int t, int d, int Dp) { return kv_value_at(t, d, Dp); }
 static KvView view(const int32_t* table, const int32_t* len, const int32_t* start, int pages, int page_blocks, int max_blocks, int heads, int B) {
-    return KvView{nullptr, nullptr, table, len, start, max_blocks / page_blocks, pages, page_blocks, max_blocks, heads, 64, B};
+    return KvView{nullptr, nullptr, table, len, start, max_blocks / page_blocks, pages, page_blocks, max_blocks / page_blocks, max_blocks, heads, 64, B};
 }
 extern "C" int block(const int32_t* row, int pages, int page_blocks, int max_blocks, int heads, int blk, int h) {
     return view(row, nullptr, nullptr, pages, page_blocks, max_blocks, heads, 1).block(row, blk, h);
