@@ -7,6 +7,8 @@
 #include "bitnet_internal.hpp"
 #include "kv_layout.hpp"
 
+#include <type_traits>
+
 namespace bitnet {
 namespace {
 
@@ -19,67 +21,127 @@ struct RopeShape {
 
 struct Turn { float cos, sin; };
 
+// cos and sin of pos * freq.  The fraction of a turn is taken in 64 bits and brought to within an eighth of the nearest quarter;
+// there the Taylor polynomials of degree 9 and 8 are within 2^-25 (their next terms, (pi / 4)^11 / 11! and (pi / 4)^10 / 10!, are below 2.5e-8),
+// and the quarter says which of the two is which and with what sign.
 __device__ inline Turn turn_of(int pos, float freq) {
-    double t = (double)pos * (double)freq * 0.15915494309189533577;
+    double t = (double)pos * ((double)freq * 0.15915494309189533577);
     t -= rint(t);
-    Turn r;
-    sincospif(2.0f * (float)t, &r.sin, &r.cos);
-    return r;
+    const double k = rint(4.0 * t);                        // -2 ... 2
+    const float x = (float)(t - 0.25 * k) * 6.28318530718f, z = x * x;
+    float s = __builtin_fmaf(z, 1.0f / 362880.0f, -1.0f / 5040.0f), c = __builtin_fmaf(z, 1.0f / 40320.0f, -1.0f / 720.0f);
+    s = __builtin_fmaf(z, s, 1.0f / 120.0f);
+    c = __builtin_fmaf(z, c, 1.0f / 24.0f);
+    s = __builtin_fmaf(z, s, -1.0f / 6.0f);
+    c = __builtin_fmaf(z, c, -0.5f);
+    s = __builtin_fmaf(x * z, s, x);
+    c = __builtin_fmaf(z, c, 1.0f);
+    const int q = (int)k;
+    const float a = q & 1 ? s : c, b = q & 1 ? c : s;      // of quarter 1: cos -> -sin, sin -> cos
+    return {(q + 1) & 2 ? -a : a, q & 2 ? -b : b};
 }
 
-// eight consecutive elements from an address of any alignment, `count` of them (the others are zero)
+// Eight consecutive elements as they stand in memory, from an address of any alignment; `count` of them exist (the others are zero).
+template <bool kBf16> struct Eight { uint4 w[kBf16 ? 1 : 2]; };
 template <bool kBf16>
-__device__ inline void load8(float (&x)[8], const void* base, int64_t at, int count) {
-    if (kBf16) {
-        const uint16_t* p = static_cast<const uint16_t*>(base) + at;
-        uint16_t u[8] = {};
-        if (count >= 8) __builtin_memcpy(u, p, 16);
-        else
+__device__ inline Eight<kBf16> load8(const void* base, int64_t at, int count) {
+    using E = std::conditional_t<kBf16, uint16_t, uint32_t>;
+    const E* p = static_cast<const E*>(base) + at;
+    E u[8] = {};
+    if (count >= 8) __builtin_memcpy(u, p, sizeof u);
+    else
 #pragma unroll
-            for (int i = 0; i < 7; ++i) if (i < count) u[i] = p[i];
+        for (int i = 0; i < 7; ++i) if (i < count) u[i] = p[i];
+    Eight<kBf16> r;
+    __builtin_memcpy(&r, u, sizeof u);
+    return r;
+}
+template <bool kBf16>
+__device__ inline void floats_of(float (&x)[8], const Eight<kBf16>& r) {
+    if constexpr (kBf16) {
+        const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(u[i]);
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
     } else {
-        const float* p = static_cast<const float*>(base) + at;
-        if (count >= 8) __builtin_memcpy(x, p, 32);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = i < count ? p[i] : 0.0f;
+        __builtin_memcpy(x, &r, sizeof x);
     }
 }
 
 __device__ inline uint4 pack8(const float (&x)[8]) {
-    uint32_t w[4];
+    typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+    v8bf w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)f32_to_bf16(x[2 * i]) | (uint32_t)f32_to_bf16(x[2 * i + 1]) << 16;
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 8; ++i) w[i] = (__bf16)x[i];       // to the nearest, ties to even
+    return __builtin_bit_cast(uint4, w);
 }
 
-// The partners of dims d0 ... d0 + 7: what the sine multiplies, with its sign.
-template <bool kBf16>
-__device__ inline void partners(float (&y)[8], const float (&x)[8], const void* base, int64_t head, int d0, const RopeShape& s) {
-    if (s.pairs) {
+// A slot: dims d0 ... d0 + 7 of a head with what they are turned with, requested before any of it is used.  Dims that are turned across a
+// multiple of eight have partners in both directions.  Reads reach up to seven elements behind a head of queries or keys,
+// where the row goes on: values follow.
+enum class Turned { Split, Pairs, Any };
+template <bool kBf16, Turned kTurned>
+struct Slot {
+    Eight<kBf16> own, low, high;       // low: partners of the dims of the lower half; Split: those alone
+    __device__ void load(const void* base, int64_t head, int d0, int D, bool turned, const RopeShape& s) {
+        own = load8<kBf16>(base, head + d0, D - d0);
+        const int half = s.rotary >> 1;
+        if (kTurned == Turned::Split) {
+            if (d0 < half) low = load8<kBf16>(base, head + d0 + half, 8);
+        } else if (kTurned == Turned::Any && turned && d0 < s.rotary) {
+            if (d0 < half) low = load8<kBf16>(base, head + d0 + half, 8);
+            if (d0 + 8 > half) {
+                // in front of the tensor there is nothing: eight elements from its first one on, moved up
+                const int64_t at = head + d0 - half;
+                high = load8<kBf16>(base, at < 0 ? 0 : at, 8);
+                if (at < 0) {
+                    using E = std::conditional_t<kBf16, uint16_t, uint32_t>;
+                    E u[8], v[8];
+                    __builtin_memcpy(u, &high, sizeof u);
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) { y[i] = -x[i + 1]; y[i + 1] = x[i]; }
-        return;
-    }
-    const int half = s.rotary >> 1;
-    if (d0 + 8 <= half || (d0 >= half && d0 + 8 <= s.rotary)) {
-        const bool low = d0 < half;
-        load8<kBf16>(y, base, head + (low ? d0 + half : d0 - half), 8);
-        if (low)
+                    for (int i = 0; i < 8; ++i) {
+                        v[i] = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = -y[i];
-        return;
+                        for (int k = 0; k < 8; ++k) if (i + at == k) v[i] = u[k];
+                    }
+                    __builtin_memcpy(&high, v, sizeof v);
+                }
+            }
+        }
     }
+    // x: own dims turned; y (Split): the partners, turned
+    __device__ void turn(float (&x)[8], float (&y)[8], int d0, bool turned, const Turn (&t)[8], const RopeShape& s) const {
+        floats_of<kBf16>(x, own);
+        const int half = s.rotary >> 1;
+        if (kTurned == Turned::Split) {
+            if (d0 < half) floats_of<kBf16>(y, low);
+            if (!turned || d0 >= half) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {                  // across the middle, or past the dims that are turned
-        const int d = d0 + i;
-        float v[8];
-        load8<kBf16>(v, base, head + (d < half ? d + half : d - half), d < s.rotary ? 1 : 0);
-        y[i] = d < half ? -v[0] : v[0];
+            for (int e = 0; e < 8; ++e) {
+                const float a = x[e] * t[e].cos - y[e] * t[e].sin;
+                y[e] = y[e] * t[e].cos + x[e] * t[e].sin;
+                x[e] = a;
+            }
+            return;
+        }
+        if (!turned || d0 >= s.rotary) return;
+        if (kTurned == Turned::Pairs) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                if (d0 + e >= s.rotary) continue;
+                const float a = x[e] * t[e].cos - x[e + 1] * t[e].sin;
+                x[e + 1] = x[e + 1] * t[e].cos + x[e] * t[e].sin;
+                x[e] = a;
+            }
+            return;
+        }
+        float l[8], h[8];
+        floats_of<kBf16>(l, low);
+        floats_of<kBf16>(h, high);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d0 + e < s.rotary) x[e] = x[e] * t[e].cos + (d0 + e < half ? -l[e] : h[e]) * t[e].sin;
     }
-}
+};
 
 __device__ inline int pair_of(int d, const RopeShape& s) { return s.pairs ? d >> 1 : d < (s.rotary >> 1) ? d : d - (s.rotary >> 1); }
 
@@ -101,19 +163,21 @@ __global__ __launch_bounds__(kThreads) void rope_append_tokens(const void* __res
     const bool mine = unit < units;
     const int64_t row = (int64_t)b * units * D, head = row + (int64_t)unit * D;
     const int pos = kv.length(kv.kv_len[b]) - 1;
-    float x[8], y[8];
-    if (mine) load8<kBf16>(x, qkv, head + d0, D - d0);
     const bool turned = mine && unit < s.heads + kv.kv_heads;
-    if (turned && d0 < s.rotary) partners<kBf16>(y, x, qkv, head, d0, s);
+    Slot<kBf16, Turned::Any> slot;
+    if (mine) slot.load(qkv, head, d0, D, turned && !s.pairs, s);
     for (int i = threadIdx.x; i < s.rotary >> 1; i += kThreads) turns[i] = turn_of(pos, inv_freq[i]);
     __syncthreads();
-    if (turned) {
+    float x[8], none[8];
+    Turn by[8];
+    if (turned)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (d0 + i < s.rotary) {
-                const Turn t = turns[pair_of(d0 + i, s)];
-                x[i] = x[i] * t.cos + y[i] * t.sin;
-            }
+        for (int e = 0; e < 8; ++e) by[e] = d0 + e < s.rotary ? turns[pair_of(d0 + e, s)] : Turn{1.0f, 0.0f};
+    if (s.pairs) {
+        const Slot<kBf16, Turned::Pairs> p{slot.own, {}, {}};
+        p.turn(x, none, d0, turned, by, s);
+    } else {
+        slot.turn(x, none, d0, turned, by, s);
     }
     if (!mine) return;
     const uint4 w = pack8(x);
@@ -137,14 +201,18 @@ __global__ __launch_bounds__(kThreads) void rope_append_tokens(const void* __res
     }
 }
 
-// Runs of new tokens: a workgroup takes the new tokens of one cache block (32 positions) and `per` heads of their rows.  Its threads keep
-// their token and dims over the heads, so that sines and cosines are computed once and stay in registers.  Values are turned
+// Runs of new tokens: a workgroup takes the new tokens of one cache block (32 positions) and `per` heads of their rows.  A thread keeps
+// its token and dims over the heads, so that sines and cosines are computed once and stay in registers.  Values are turned
 // over through LDS: the cache holds eight tokens of a dim together.
-template <bool kBf16>
+//
+// What a thread takes of a head is a slot: eight dims, or where the halves that are turned together begin at multiples of eight (Split)
+// eight of the lower half and their eight partners, each of which is read once.
+template <bool kBf16, Turned kTurned, int kM /* slots a thread */>
 __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, KvView kv,
                                                                RopeShape s, int per, uint16_t* __restrict__ q) {
-    constexpr int kMost = 256 / 8 * kKvBlock / kThreads;       // pieces of eight dims a thread at most: four
-    __shared__ uint16_t tile[kKvBlock * (256 + 2)];
+    constexpr int kPitch = 256 + 8;
+    __shared__ uint4 tile4[kTurned == Turned::Any ? kKvBlock * 128 / 2 : kKvBlock * kPitch / 8];      // Any: sines and cosines first
+    uint16_t* tile = reinterpret_cast<uint16_t*>(tile4);
     const int D = kv.D, Dp = kv_padded_dim(D), quads = Dp >> 3, units = s.heads + 2 * kv.kv_heads;
     const int b = sequence_of_tile(kv.q_start, kv.B, blockIdx.x, 1, kKvBlock, 2);
     const NewTokens nt(kv, b, s.T);
@@ -156,51 +224,70 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
     const int t0 = max(nt.pos0 - blk * kKvBlock, 0), t1 = min(nt.pos0 + nt.n - blk * kKvBlock, kKvBlock);     // the block's new tokens
     const int row0 = nt.first + blk * kKvBlock - nt.pos0;      // of token 0 of the block
     const int u0 = blockIdx.y * per, u1 = min(u0 + per, units);
+    // the page: its number is the same for all heads
+    const int page_index = blk >= 0 ? blk / kv.page_blocks : 0, page = blk >= 0 ? kv.table[b * kv.table_stride + page_index] : -1;
 
-    int tok[kMost], d0[kMost];
-    Turn turn[kMost][8];
+    const int half8 = s.rotary >> 4;                           // Split: quads of a half
+    const int slots = kTurned == Turned::Split ? quads - half8 : quads, tiles = (slots + 7) >> 3;
+    int tok[kM], d0[kM];
+    Turn turn[kM][8];
 #pragma unroll
-    for (int m = 0; m < kMost; ++m) {
-        // eight pieces of a row next to each other, then eight tokens: 128 bytes of a bf16 row at a time
-        const int i = threadIdx.x + m * kThreads, tiles = (quads + 7) >> 3;
-        const int j = (i & 7) + 8 * ((i >> 6) % tiles);
+    for (int m = 0; m < kM; ++m) {
+        // eight slots of a row next to each other, then eight tokens: 128 bytes of a bf16 row at a time
+        const int i = threadIdx.x + m * kThreads, j = (i & 7) + 8 * ((i >> 6) % tiles);
         tok[m] = ((i >> 3) & 7) + 8 * ((i >> 6) / tiles);
-        d0[m] = 8 * j;
-        if (j >= quads || tok[m] < t0 || tok[m] >= t1) tok[m] = -1;
-        if (tok[m] >= 0 && u0 < s.heads + kv.kv_heads)
+        if (j >= slots || tok[m] < t0 || tok[m] >= t1) tok[m] = -1;
+        // Split: the lower half's quads, then those that are not turned
+        d0[m] = 8 * (kTurned == Turned::Split && j >= half8 ? j + half8 : j);
+        if (kTurned != Turned::Any && tok[m] >= 0 && u0 < s.heads + kv.kv_heads)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (s.pairs && (e & 1)) { turn[m][e] = turn[m][e - 1]; continue; }
+                if (kTurned == Turned::Pairs && (e & 1)) { turn[m][e] = turn[m][e - 1]; continue; }
                 turn[m][e] = d0[m] + e < s.rotary ? turn_of(blk * kKvBlock + tok[m], inv_freq[pair_of(d0[m] + e, s)]) : Turn{1.0f, 0.0f};
             }
     }
+    if (kTurned == Turned::Any && u0 < s.heads + kv.kv_heads) {      // two dims have an angle: computed once, taken twice
+        Turn* table = reinterpret_cast<Turn*>(tile4);
+        const int half = s.rotary >> 1;
+        for (int i = threadIdx.x; i < kKvBlock * half; i += kThreads) table[i] = turn_of(blk * kKvBlock + i / half, inv_freq[i % half]);
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < kM; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (tok[m] >= 0 && d0[m] + e < s.rotary) turn[m][e] = table[tok[m] * half + pair_of(d0[m] + e, s)];
+        __syncthreads();
+    }
+    Slot<kBf16, kTurned> slot[kM], next[kM];
+    auto request = [&](Slot<kBf16, kTurned> (&x)[kM], int u) {
+#pragma unroll
+        for (int m = 0; m < kM; ++m)
+            if (tok[m] >= 0) x[m].load(qkv, ((int64_t)(row0 + tok[m]) * units + u) * D, d0[m], D, u < s.heads + kv.kv_heads, s);
+    };
+    request(next, u0);
+#pragma unroll 1
     for (int u = u0; u < u1; ++u) {
+#pragma unroll
+        for (int m = 0; m < kM; ++m) slot[m] = next[m];
+        if (u + 1 < u1) request(next, u + 1);
         const bool query = u < s.heads, key = !query && u < s.heads + kv.kv_heads;
         int block = -1;
-        if (!query && blk >= 0) block = kv.block(kv.table + b * kv.table_stride, blk, key ? u - s.heads : u - s.heads - kv.kv_heads);
+        if (!query) block = kv.block_on(page, blk - page_index * kv.page_blocks, key ? u - s.heads : u - s.heads - kv.kv_heads);
         if (!query && block < 0) continue;                     // the same for the whole workgroup
         const int64_t at = (int64_t)block * kKvBlock * Dp;
 #pragma unroll
-        for (int m = 0; m < kMost; ++m) {
+        for (int m = 0; m < kM; ++m) {
             if (tok[m] < 0) continue;
-            const int64_t r = row0 + tok[m], head = (r * units + u) * D;
-            float x[8];
-            load8<kBf16>(x, qkv, head + d0[m], D - d0[m]);
-            if (query || key) {
-                if (d0[m] < s.rotary) {
-                    float y[8];
-                    partners<kBf16>(y, x, qkv, head, d0[m], s);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (d0[m] + e < s.rotary) x[e] = x[e] * turn[m][e].cos + y[e] * turn[m][e].sin;
-                }
-                const uint4 w = pack8(x);
-                if (query) store_any(q + (r * s.heads + u) * D + d0[m], w, D - d0[m]);
-                else *reinterpret_cast<uint4*>(kv.k + at + kv_key_at(tok[m], d0[m])) = w;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) tile[tok[m] * (256 + 2) + d0[m] + e] = f32_to_bf16(x[e]);
-            }
+            const int64_t out = ((int64_t)(row0 + tok[m]) * s.heads + u) * D;
+            auto put = [&](int d, uint4 w) {
+                if (query) store_any(q + out + d, w, D - d);
+                else if (key) *reinterpret_cast<uint4*>(kv.k + at + kv_key_at(tok[m], d)) = w;
+                else *reinterpret_cast<uint4*>(&tile[tok[m] * kPitch + d]) = w;
+            };
+            float x[8], y[8];
+            slot[m].turn(x, y, d0[m], query || key, turn[m], s);
+            put(d0[m], pack8(x));
+            if (kTurned == Turned::Split && d0[m] < 8 * half8) put(d0[m] + 8 * half8, pack8(y));
         }
         if (query || key) continue;
         __syncthreads();
@@ -209,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
             if (8 * g + 8 <= t0 || 8 * g >= t1) continue;
             uint16_t e[8];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) e[t] = tile[(8 * g + t) * (256 + 2) + d];
+            for (int t = 0; t < 8; ++t) e[t] = tile[(8 * g + t) * kPitch + d];
             uint16_t* to = kv.v + at + (g * Dp + d) * 8;
             if (8 * g >= t0 && 8 * g + 8 <= t1) {
                 uint4 w;
@@ -222,6 +309,29 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
         }
         __syncthreads();
     }
+}
+
+template <bool kBf16, Turned kTurned>
+hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& kv, const RopeShape& s, uint16_t* q, hipStream_t stream) {
+    const int units = s.heads + 2 * kv.kv_heads, quads = kv_padded_dim(kv.D) / 8;
+    const int slots = kTurned == Turned::Split ? quads - (s.rotary >> 4) : quads, m = (slots + 7) / 8;
+    const int64_t tiles = tiles_at_most(s.T, kv.B, 1, kKvBlock, 2);
+    // Heads of a workgroup: four share a token's sines and cosines and the loads that say where its row and its page are, if that leaves
+    // three workgroups for each CU, and fewer otherwise (us, one / two / four / eight: 4096 tokens, 64 heads over 8, two prompts 65 /
+    // 49 / 40 / 41; 512 tokens 10.8 / 9.0 / 10.2 / 15.3; 77 tokens 5.2 / 5.5 / 6.8 / 11.2).
+    const int64_t all = tiles * units / 768;
+    const int per = (int)(all < 1 ? 1 : all > 4 ? 4 : all);
+    const dim3 grid((unsigned)tiles, (unsigned)ceil_div(units, per));
+    if (m == 1) rope_append_blocks<kBf16, kTurned, 1><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
+    else if (m == 2) rope_append_blocks<kBf16, kTurned, 2><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
+    else rope_append_blocks<kBf16, kTurned, 4><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
+    return hipGetLastError();
+}
+template <bool kBf16>
+hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& kv, const RopeShape& s, uint16_t* q, hipStream_t stream) {
+    if (s.pairs) return launch_blocks<kBf16, Turned::Pairs>(qkv, inv_freq, kv, s, q, stream);
+    if (s.rotary % 16 == 0) return launch_blocks<kBf16, Turned::Split>(qkv, inv_freq, kv, s, q, stream);
+    return launch_blocks<kBf16, Turned::Any>(qkv, inv_freq, kv, s, q, stream);
 }
 
 }  // namespace
@@ -237,12 +347,7 @@ hipError_t launch_rope_append(const void* qkv, bool bf16, const float* inv_freq,
         else rope_append_tokens<false><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, quads, qo);
         return hipGetLastError();
     }
-    const int64_t tiles = tiles_at_most(T, kv.B, 1, kKvBlock, 2);
-    const int per = (int)(tiles * units <= 1024 ? 1 : tiles * units >= 8192 ? 8 : ceil_div(tiles * units, 1024));
-    const dim3 grid((unsigned)tiles, (unsigned)ceil_div(units, per));
-    if (bf16) rope_append_blocks<true><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, qo);
-    else rope_append_blocks<false><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, qo);
-    return hipGetLastError();
+    return bf16 ? launch_blocks<true>(qkv, inv_freq, kv, s, qo, stream) : launch_blocks<false>(qkv, inv_freq, kv, s, qo, stream);
 }
 
 }  // namespace bitnet
