@@ -85,6 +85,15 @@ __device__ inline void weights_pair(v8bf* w, int j, float p0, float p1) {
     }
 }
 
+// The sum of a row's weights is a product with ones: it takes them as the values' product does, rounded, so that the
+// rounding of a weight that outweighs the others is in both and goes out of their quotient, and it takes no vector instructions.  Every lane of a query's four groups gets it, in all four places.
+__device__ inline v8bf ones_operand() {
+    v8bf w;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = (__bf16)1.0f;
+    return w;
+}
+
 // Which of a lane's eight consecutive values of a dim belong to a token in front of `count`: the others are whatever the memory
 // held, and a weight of zero does not make a NaN nothing.
 __device__ inline void values_keep(v4u& v, int count) {

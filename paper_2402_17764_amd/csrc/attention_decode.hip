@@ -53,10 +53,11 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
 #pragma unroll
     for (int i = 0; i < kV; ++i) voff[i] = (g * Dp + (kExact || i < 2 * kWholeChunks ? 16 * i + r : min(16 * i + r, Dp - 1))) * 16;
 
-    v4f acc[kV];
+    v4f acc[kV], l = {0, 0, 0, 0};                         // l: the sum of the weights, four times
 #pragma unroll
     for (int i = 0; i < kV; ++i) acc[i] = (v4f){0, 0, 0, 0};
-    float m = kMinusInf, l = 0.0f;                         // l: of this lane's tokens
+    float m = kMinusInf;
+    const v8bf ones = ones_operand();
 
     struct Block { v4u k[kC][2], v[kV]; };
     // this wave's blocks are first, first + kW, ...; their numbers in the cache stand in the lanes, 64 at a time
@@ -106,13 +107,12 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
         }
         const float base = m == kMinusInf ? 0.0f : m * a.scale;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            p[j] = exp2_fast(__builtin_fmaf(p[j], a.scale, -base));
-            l += p[j];
-        }
+        for (int j = 0; j < 8; ++j) p[j] = exp2_fast(__builtin_fmaf(p[j], a.scale, -base));
         v8bf w[kF32 ? 3 : 1];
 #pragma unroll
         for (int j = 0; j < 8; j += 2) weights_pair<kF32>(w, j, p[j], p[j + 1]);
+#pragma unroll
+        for (int e = 0; e < (kF32 ? 3 : 1); ++e) l = mfma_bf16(ones, w[e], l);
 #pragma unroll
         for (int e = 0; e < (kF32 ? 3 : 1); ++e)
 #pragma unroll
@@ -139,10 +139,9 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
     }
 
     // The waves' states into one: weights exp(m_w - m), sums by rounds of 64 dims through LDS.
-    l = groups_sum(l);
     if (g == 0) {
         maxima[wave * 16 + r] = m;
-        totals[wave * 16 + r] = l;
+        totals[wave * 16 + r] = l[0];
     }
     __syncthreads();
     float all = kMinusInf;

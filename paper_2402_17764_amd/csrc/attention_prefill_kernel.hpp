@@ -110,12 +110,13 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #pragma unroll
     for (int i = 0; i < kV; ++i) voff[i] = (g * Dp + (kExact || i < 2 * whole_chunks(kC) ? 16 * i + r : min(16 * i + r, Dp - 1))) * 16;
 
-    v4f acc[kNT][kV];
-    float m[kNT], l[kNT];
+    v4f acc[kNT][kV], l[kNT];                                              // l: the sum of the weights, four times
+    float m[kNT];
+    const v8bf ones = ones_operand();
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         m[n] = kMinusInf;
-        l[n] = 0.0f;
+        l[n] = (v4f){0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kV; ++i) acc[n][i] = (v4f){0, 0, 0, 0};
     }
@@ -142,8 +143,6 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 const int n = q / 4, j = q % 4 * 2;
                 const float p0 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][j & 3], a.scale, -base[n]));
                 const float p1 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][(j & 3) + 1], a.scale, -base[n]));
-                l[n] += p0;
-                l[n] += p1;
                 weights_pair<kF32>(w[u][n], j, p0, p1);
             }
         };
@@ -158,7 +157,14 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
+        auto sum = [&](int u) {
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int e = 0; e < kParts; ++e) l[n] = mfma_bf16(ones, w[u][n][e], l[n]);
+        };
         auto product = [&](int u, int with) {
+            sum(u);
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
                 const int f = kU * kKeys + u * kV + i;
@@ -191,6 +197,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
             }
             if (__builtin_amdgcn_ballot_w64(passed)) {
                 if (u > 0) {
+                    sum(u - 1);
 #pragma unroll
                     for (int i = 0; i < kV; ++i) {
                         const v8bf v = *reinterpret_cast<const v8bf*>(values + (u - 1) * piece + voff[i]);
@@ -293,7 +300,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
-        const float total = groups_sum(l[n]), inv = total > 0.0f ? 1.0f / total : 0.0f;
+        const float total = l[n][0], inv = total > 0.0f ? 1.0f / total : 0.0f;
         if (out_row[n] < 0) continue;
         const int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
         const bool whole = run >= all_stages;
