@@ -3,7 +3,9 @@ against its definition in 64 bits (attention_ref.py), with bounds derived there,
 import numpy as np
 import pytest
 
+import oracle
 from attention_ref import BF16_HALF_STEP, Cache, attention, bf16, rope
+from paper_2402_17764_amd import synth
 
 pytestmark = pytest.mark.gpu
 
@@ -390,3 +392,147 @@ def test_prompt_then_tokens_in_a_graph(gpu_lib):
         for t in range(total[b]):
             o, bounds = attention(queries[b][t], keys, values, np.arange(total[b]) <= t, D ** -0.5)
             assert np.all(np.abs(out[b][t] - o) <= bounds[1]), (b, t)
+
+
+def test_a_decoder_layers_attention_half(gpu_lib):
+    """norm -> Q | K | V -> rotary, cache -> attention -> output projection, a ragged prompt and then a token, heads of 100: the library's own
+    products in front and behind.  What the products give is the oracle's (bit for bit up to the output's bf16), what stands
+    between them is held to its definition on the rows that the device computed."""
+    heads, D, P = 4, 100, 32
+    H = heads * D
+    wqkv, wo = synth.weights(3 * H, H, config=1, layer=3), synth.weights(H, H, config=1, layer=4)
+    packed, gamma = gpu_lib.quantize_weights_segmented(torch.from_numpy(wqkv).cuda(), [H, H, H])
+    packed_o, gamma_o = gpu_lib.quantize_weights(torch.from_numpy(wo).cuda())
+    freq = (10000.0 ** (-np.arange(0, D, 2) / D)).astype(np.float32)
+    f = dev(freq, np.float32)
+    rng = np.random.default_rng(33)
+    table, pages = tables(rng, 2, 4)
+    tab = dev(table)
+    k, v = gpu_lib.kv_cache(pages, P, heads, D)
+    done, keys, values = [0, 0], [np.zeros((0, heads, D))] * 2, [np.zeros((0, heads, D))] * 2
+    for chunk in ([40, 70], [3, 0], [1, 1]):
+        T = sum(chunk)
+        x = torch.from_numpy(synth.activations(T, H, config=1, layer=T)).cuda().to(torch.bfloat16)
+        lens, start = [done[b] + chunk[b] for b in range(2)], np.cumsum([0] + chunk)
+        one = chunk == [1, 1]
+        if one:
+            qkv = gpu_lib.rmsnorm_linear_fused(x, None, 1e-6, packed, gamma, 3 * H, y_dtype=gpu_lib.BF16, segmented=True)
+            q = gpu_lib.rope_kv_append(qkv, f, k, v, tab, dev(lens), heads)
+            y = gpu_lib.attention_decode(q, k, v, tab, dev(lens))
+            out = gpu_lib.linear_fused(y, packed_o, gamma_o, H)
+        else:
+            qkv = gpu_lib.linear_segmented(*gpu_lib.rmsnorm_quantize(x), packed, gamma, 3 * H, y_dtype=gpu_lib.BF16)
+            q = gpu_lib.rope_kv_append(qkv, f, k, v, tab, dev(lens), heads, q_start=dev(start))
+            y = gpu_lib.attention_prefill(q, k, v, tab, dev(lens), dev(start))
+            out = gpu_lib.linear(*gpu_lib.quantize_acts(y), packed_o, gamma_o, H)
+        rows = host(qkv).reshape(T, 3 * heads, D)
+        hk, hv = Cache(pages, P, heads, D).from_layout(host(k), host(v))
+        cache = Cache(pages, P, heads, D)
+        cache.k, cache.v = hk, hv
+        for b in range(2):
+            r, pos = slice(int(start[b]), int(start[b + 1])), np.arange(done[b], lens[b])
+            turned, off = rope(rows[r, : 2 * heads], pos, freq, False)
+            got_k, got_v, _ = cache.get(table[b], lens[b])
+            assert np.array_equal(got_v[done[b]:], rows[r, 2 * heads:])
+            assert np.all(np.abs(got_k[done[b]:] - turned[:, heads:]) <= off[:, heads:] * 1.01 + BF16_HALF_STEP * np.abs(turned[:, heads:]))
+            assert np.array_equal(got_k[: done[b]], keys[b]) and np.array_equal(got_v[: done[b]], values[b])      # earlier tokens stay
+            qs = host(q)[r]
+            assert np.all(np.abs(qs - turned[:, :heads]) <= off[:, :heads] * 1.01 + BF16_HALF_STEP * np.abs(turned[:, :heads]))
+            for i in range(chunk[b]):
+                o, bounds = attention(qs[i], got_k, got_v, np.arange(lens[b]) <= pos[i], D ** -0.5)
+                assert np.all(np.abs(host(y)[int(start[b]) + i].reshape(heads, D) - o) <= bounds[0])
+            keys[b], values[b], done[b] = got_k, got_v, lens[b]
+        ref = oracle.bitlinear(y.float().cpu().numpy(), wo)
+        nz = ref["y"] != 0
+        assert (np.abs(host(out)[nz] - ref["y"][nz]) / np.abs(ref["y"][nz])).max() <= 1e-5
+
+
+@pytest.mark.parametrize("D", [36, 256])
+def test_runs_captured_without_a_call_in_front(gpu_lib, D):
+    """The first launch of a head's size in the process is into a graph; its replays, with other keys and lengths in place, are eager calls'."""
+    batch = Batch([1300, 90], 32, 2, D, 14)
+    q, y = dev16(batch.queries(50, 4, D)), torch.zeros((50, 4 * D), dtype=torch.float32, device="cuda")
+    lens, start, tab = dev([1300, 90]), dev([0, 7, 50]), dev(batch.table)
+    ws = torch.empty(max(1, gpu_lib.attention_workspace(50, 4, D, batch.k, tab, prefill=True)), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        gpu_lib.attention_prefill(q, batch.k, batch.v, tab, lens, start, y_dtype=gpu_lib.F32, y=y, workspace=ws)
+    for n in ([1300, 90], [700, 44], [1299, 89], [0, 43]):
+        lens.copy_(dev(n))
+        q.neg_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, gpu_lib.attention_prefill(q, batch.k, batch.v, tab, lens, start, y_dtype=gpu_lib.F32))
+        check_attention(host(y), host(q), batch, [(0, n[0] - 7 + i) for i in range(7)] + [(1, n[1] - 43 + i) for i in range(43)], D ** -0.5, True)
+
+
+def test_two_streams_with_workspaces_of_their_own(gpu_lib):
+    batches = [Batch([3000, 2900], 64, 2, 128, 15), Batch([2500, 1100], 64, 2, 128, 16)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    qs = [dev16(b.queries(2, 8, 128)) for b in batches]
+    tabs, lens = [dev(b.table) for b in batches], [dev(b.lens) for b in batches]
+    want = [gpu_lib.attention_decode(qs[i], b.k, b.v, tabs[i], lens[i], y_dtype=gpu_lib.F32) for i, b in enumerate(batches)]
+    ws = [torch.empty(gpu_lib.attention_workspace(2, 8, 128, b.k, tabs[i]), dtype=torch.uint8, device="cuda") for i, b in enumerate(batches)]
+    assert all(w.numel() for w in ws)
+    got = [[torch.empty_like(want[i]) for _ in range(20)] for i in range(2)]
+    torch.cuda.synchronize()
+    for j in range(20):
+        for i, b in enumerate(batches):
+            with torch.cuda.stream(streams[i]):
+                gpu_lib.attention_decode(qs[i], b.k, b.v, tabs[i], lens[i], y_dtype=gpu_lib.F32, y=got[i][j], workspace=ws[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[i][j], want[i]) for i in range(2) for j in range(20))
+
+
+@pytest.mark.parametrize("prefill", [False, True])
+def test_with_and_without_a_workspace(gpu_lib, prefill):
+    """No workspace, one that is too small, and the query's: the same values up to the order of sums."""
+    lens = [1500, 800]
+    batch = Batch(lens, 64, 2, 128, 17)
+    q = batch.queries(2, 8, 128)
+    tab = dev(batch.table)
+    need = gpu_lib.attention_workspace(2, 8, 128, batch.k, tab, prefill=prefill)
+    assert need > 0
+    for n in (0, need - 16, need, need + 48):
+        ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        if prefill:
+            y = gpu_lib.attention_prefill(dev16(q), batch.k, batch.v, tab, dev(lens), dev([0, 1, 2]), y_dtype=gpu_lib.F32, workspace=ws)
+        else:
+            y = gpu_lib.attention_decode(dev16(q), batch.k, batch.v, tab, dev(lens), y_dtype=gpu_lib.F32, workspace=ws)
+        check_attention(host(y), q, batch, [(0, 1499), (1, 799)], 128 ** -0.5, True, "%d of %d bytes" % (n, need))
+
+
+def test_refusals_of_the_binding(gpu_lib):
+    batch = Batch([40, 33], 32, 2, 64, 18)
+    tab, lens, q = dev(batch.table), dev([40, 33]), dev16(batch.queries(2, 4, 64))
+    start = dev([0, 1, 2])
+    ok = dict(q=q, k_cache=batch.k, v_cache=batch.v, page_table=tab, kv_len=lens)
+    gpu_lib.attention_decode(**ok)
+    wrong = [("q", q.float(), TypeError), ("q", q[0], ValueError), ("q", q[:1], ValueError), ("q", q.transpose(0, 1), ValueError), ("q", q[:, :3].contiguous(), gpu_lib.BitnetError),
+             ("q", q[..., :32].contiguous(), ValueError), ("k_cache", batch.k.float(), TypeError), ("k_cache", batch.k[0], ValueError), ("v_cache", batch.v[:-1], ValueError),
+             ("v_cache", batch.k, ValueError), ("page_table", tab.long(), TypeError), ("page_table", tab.t(), ValueError), ("page_table", tab[0], ValueError),
+             ("kv_len", lens[:1], ValueError), ("kv_len", lens.long(), TypeError), ("scale", 0.0, gpu_lib.BitnetError), ("scale", float("nan"), gpu_lib.BitnetError),
+             ("y_dtype", gpu_lib.I32, ValueError), ("y_dtype", 9, KeyError), ("y", torch.empty((2, 255), dtype=torch.bfloat16, device="cuda"), ValueError),
+             ("y", torch.empty((2, 256), dtype=torch.float32, device="cuda"), TypeError)]
+    for name, value, error in wrong:
+        for call, more in ((gpu_lib.attention_decode, {}), (gpu_lib.attention_prefill, {"q_start": start})):
+            if call is gpu_lib.attention_prefill and name == "q" and value.dim() == 3 and value.shape[0] == 1:
+                continue                                     # one row for two sequences is a batch of runs like any other
+            with pytest.raises(error):
+                call(**{**ok, **more, name: value})
+    for bad, error in ((start[:2], ValueError), (start.long(), TypeError), (None, gpu_lib.BitnetError)):
+        with pytest.raises(error):
+            gpu_lib.attention_prefill(**ok, q_start=bad)
+    qkv, f = torch.zeros((2, 8 * 64), device="cuda"), torch.ones(32, device="cuda")
+    args = dict(qkv=qkv, inv_freq=f, k_cache=batch.k, v_cache=batch.v, page_table=tab, kv_len=lens, heads=4)
+    gpu_lib.rope_kv_append(**args)
+    for name, value, error in [("qkv", qkv.half(), TypeError), ("qkv", qkv[0], ValueError), ("qkv", qkv[:, :500].contiguous(), ValueError), ("qkv", qkv[:1], gpu_lib.BitnetError),
+                               ("heads", 3, ValueError), ("heads", 0, ValueError), ("heads", -4, ValueError), ("inv_freq", f.double(), TypeError), ("inv_freq", f[None], ValueError),
+                               ("inv_freq", torch.ones(33, device="cuda"), gpu_lib.BitnetError), ("q", torch.empty((2, 4, 63), dtype=torch.bfloat16, device="cuda"), ValueError),
+                               ("q_start", start[:2], ValueError)]:
+        with pytest.raises(error):
+            gpu_lib.rope_kv_append(**{**args, name: value})
+    for bad in ((0, 32, 1, 64), (4, 40, 1, 64), (4, 32, 1, 63), (4, 32, 1, 258)):
+        with pytest.raises(gpu_lib.BitnetError):
+            gpu_lib.kv_cache(*bad)
