@@ -10,7 +10,8 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
-// Of a head's kC chunks of 32 dims as the kernels are built (1, 2, 3, 4, 6 or 8), how many are whole for every head that takes them.
+// The sizes of heads that the kernels are built for: kC chunks of 32 dims for the scores, kV tiles of 16 for the values.  Exact: all of them are
+// whole.  Otherwise the last may be filled in part -- kWhole chunks are not -- and up to 128 dims the last chunk has one tile or two.
 constexpr int whole_chunks(int kC) { return kC <= 4 ? kC - 1 : kC - 2; }
 
 constexpr float kMinusInf = -__builtin_inff();

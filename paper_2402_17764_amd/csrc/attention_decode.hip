@@ -22,9 +22,8 @@ struct DecodeArgs {
 
 // A row is 16 query heads (or what a group has left) of one key-value head of one sequence.  Its blocks are dealt out to up to
 // parts.splits workgroups (blockIdx.y).
-template <int kC, bool kExact, bool kF32, int kW>
+template <int kC, int kV, bool kExact, bool kF32, int kW>
 __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_rows(DecodeArgs a, Parts parts, KvView kv) {
-    constexpr int kV = 2 * kC;                             // tiles of 16 dims
     constexpr int kWholeChunks = whole_chunks(kC);
     constexpr int kRound = kV < 4 ? kV : 4;                // tiles that the waves add up at a time
     constexpr int kPitch = 16 * kRound + 4;
@@ -189,11 +188,11 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
     }
 }
 
-template <int kC, bool kExact>
+template <int kC, int kV, bool kExact>
 hipError_t launch_decode(const DecodeArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream) {
     const dim3 grid((unsigned)((int64_t)kv.B * kv.kv_heads * a.column_tiles), parts.splits);
-    if (f32) attention_decode_rows<kC, kExact, true, 4><<<grid, 256, 0, stream>>>(a, parts, kv);
-    else attention_decode_rows<kC, kExact, false, 4><<<grid, 256, 0, stream>>>(a, parts, kv);
+    if (f32) attention_decode_rows<kC, kV, kExact, true, 4><<<grid, 256, 0, stream>>>(a, parts, kv);
+    else attention_decode_rows<kC, kV, kExact, false, 4><<<grid, 256, 0, stream>>>(a, parts, kv);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || parts.splits < 2) return e;
     return launch_attention_join({a.o, a.scale, a.heads, a.group, kv.B, 0}, parts, kv, f32, stream);
@@ -232,15 +231,15 @@ hipError_t launch_attention_decode(const void* q, const KvView& kv, int heads, f
     const Splits s = decode_splits(kv, heads);
     if (s.n > 1 && workspace_bytes >= attention_decode_workspace_bytes(kv, heads)) parts = Parts(workspace, (int64_t)kv.B * heads, s.n, s.least, kv.D);
     const int chunks = (int)ceil_div(kv.D, 32);
-    const bool exact = kv.D % 32 == 0;
-#define DECODE(kC_) return exact && chunks == kC_ ? launch_decode<kC_, true>(a, parts, kv, f32, stream) : launch_decode<kC_, false>(a, parts, kv, f32, stream)
+    const bool exact = kv.D % 32 == 0, one_tile = kv.D % 32 != 0 && kv.D % 32 <= 16;
+#define DECODE(kC_, kV_, kE_) return launch_decode<kC_, kV_, kE_>(a, parts, kv, f32, stream)
     switch (chunks) {
-        case 1: DECODE(1);
-        case 2: DECODE(2);
-        case 3: DECODE(3);
-        case 4: DECODE(4);
-        case 5: case 6: DECODE(6);
-        default: DECODE(8);
+        case 1: if (exact) DECODE(1, 2, true); if (one_tile) DECODE(1, 1, false); DECODE(1, 2, false);
+        case 2: if (exact) DECODE(2, 4, true); if (one_tile) DECODE(2, 3, false); DECODE(2, 4, false);
+        case 3: if (exact) DECODE(3, 6, true); if (one_tile) DECODE(3, 5, false); DECODE(3, 6, false);
+        case 4: if (exact) DECODE(4, 8, true); if (one_tile) DECODE(4, 7, false); DECODE(4, 8, false);
+        case 5: case 6: if (exact && chunks == 6) DECODE(6, 12, true); DECODE(6, 12, false);
+        default: if (exact && chunks == 8) DECODE(8, 16, true); DECODE(8, 16, false);
     }
 #undef DECODE
 }

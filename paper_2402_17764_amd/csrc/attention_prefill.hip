@@ -3,10 +3,10 @@
 
 namespace bitnet {
 
-#define EXTERN(kC_) \
-    extern template hipError_t launch_prefill<kC_, true>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t); \
-    extern template hipError_t launch_prefill<kC_, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t)
-EXTERN(1); EXTERN(2); EXTERN(3); EXTERN(4); EXTERN(6); EXTERN(8);
+#define EXTERN(kC_, kV_, kE_) extern template hipError_t launch_prefill<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t)
+EXTERN(1, 2, true); EXTERN(2, 4, true); EXTERN(3, 6, true); EXTERN(4, 8, true); EXTERN(6, 12, true); EXTERN(8, 16, true);
+EXTERN(1, 1, false); EXTERN(2, 3, false); EXTERN(3, 5, false); EXTERN(4, 7, false);
+EXTERN(1, 2, false); EXTERN(2, 4, false); EXTERN(3, 6, false); EXTERN(4, 8, false); EXTERN(6, 12, false); EXTERN(8, 16, false);
 #undef EXTERN
 
 struct PrefillPlan { PrefillTile tile; int splits, least; };
@@ -42,17 +42,19 @@ hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, 
     Parts parts;
     if (plan.splits > 1 && workspace_bytes >= Parts::bytes(T * heads, plan.splits, kv.D)) parts = Parts(workspace, T * heads, plan.splits, plan.least, kv.D);
     const int chunks = (int)ceil_div(kv.D, 32);
-    const bool exact = kv.D % 32 == 0;
+    const bool exact = kv.D % 32 == 0, one_tile = !exact && kv.D % 32 <= 16;
     hipError_t e = hipErrorInvalidValue;
-#define PREFILL(kC_) e = exact && chunks == kC_ ? launch_prefill<kC_, true>(plan.tile, a, parts, kv, f32, stream) : launch_prefill<kC_, false>(plan.tile, a, parts, kv, f32, stream); break
+#define PREFILL(kC_, kV_, kE_) e = launch_prefill<kC_, kV_, kE_>(plan.tile, a, parts, kv, f32, stream)
+#define SIZES(kC_) if (exact) PREFILL(kC_, 2 * kC_, true); else if (one_tile) PREFILL(kC_, 2 * kC_ - 1, false); else PREFILL(kC_, 2 * kC_, false); break
     switch (chunks) {
-        case 1: PREFILL(1);
-        case 2: PREFILL(2);
-        case 3: PREFILL(3);
-        case 4: PREFILL(4);
-        case 5: case 6: PREFILL(6);
-        default: PREFILL(8);
+        case 1: SIZES(1);
+        case 2: SIZES(2);
+        case 3: SIZES(3);
+        case 4: SIZES(4);
+        case 5: case 6: if (exact && chunks == 6) PREFILL(6, 12, true); else PREFILL(6, 12, false); break;
+        default: if (exact && chunks == 8) PREFILL(8, 16, true); else PREFILL(8, 16, false); break;
     }
+#undef SIZES
 #undef PREFILL
     if (e != hipSuccess || parts.splits < 2) return e;
     return launch_attention_join({o, a.scale, heads, a.group, (int)T, prefill_rows(plan.tile)}, parts, kv, f32, stream);

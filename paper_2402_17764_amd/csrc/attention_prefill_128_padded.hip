@@ -1,6 +1,6 @@
-// The prefill attention kernels for heads of 98 to 126 dims.
+// The prefill attention kernels for heads of 114 to 126 dims.
 #include "attention_prefill_kernel.hpp"
 
 namespace bitnet {
-template hipError_t launch_prefill<4, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
+template hipError_t launch_prefill<4, 8, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
 }

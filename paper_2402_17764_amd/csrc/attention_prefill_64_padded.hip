@@ -1,6 +1,6 @@
-// The prefill attention kernels for heads of 34 to 62 dims.
+// The prefill attention kernels for heads of 50 to 62 dims.
 #include "attention_prefill_kernel.hpp"
 
 namespace bitnet {
-template hipError_t launch_prefill<2, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
+template hipError_t launch_prefill<2, 4, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
 }

@@ -1,6 +1,6 @@
-// The prefill attention kernels for heads of 66 to 94 dims.
+// The prefill attention kernels for heads of 82 to 94 dims.
 #include "attention_prefill_kernel.hpp"
 
 namespace bitnet {
-template hipError_t launch_prefill<3, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
+template hipError_t launch_prefill<3, 6, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
 }

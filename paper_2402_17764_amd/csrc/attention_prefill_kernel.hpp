@@ -34,10 +34,10 @@ constexpr float kSlack = 8.0f;         // in the exponent of 2
 
 constexpr int prefill_piece(int Dp) { return (Dp * 64 + 1023) / 1024 * 1024; }     // a block's keys (or values) in LDS: whole wave loads
 
-template <int kC, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
+template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
 __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(PrefillArgs a, Parts parts, KvView kv) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kV = 2 * kC, kRows = 16 * kNT * kW, kU = kStageBlocks;   // cache blocks of a stage
+    constexpr int kRows = 16 * kNT * kW, kU = kStageBlocks;   // cache blocks of a stage
     constexpr int kPerUnit = kStageTokens / (kKvBlock * kStageBlocks);
     extern __shared__ uint4 smem[];
     __shared__ int bad_at[256 + 4];                                        // of each dim: the first position whose value is not finite
@@ -322,10 +322,10 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #endif
 }
 
-template <int kC, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
+template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
 hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView& kv, hipStream_t stream) {
     static RaisedFlags raised;
-    const auto kernel = attention_prefill_tiles<kC, kExact, kNT, kStageBlocks, kW, kOcc, kF32>;
+    const auto kernel = attention_prefill_tiles<kC, kV, kExact, kNT, kStageBlocks, kW, kOcc, kF32>;
     const int lds = 2 * 2 * kStageBlocks * prefill_piece(kv_padded_dim(kv.D));
     if (lds > 65536 - 2048) {                              // with the static part
         const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(kernel), 2 * 2 * kStageBlocks * prefill_piece(32 * kC), raised);
@@ -335,16 +335,16 @@ hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView&
     kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, lds, stream>>>(a, parts, kv);
     return hipGetLastError();
 }
-template <int kC, bool kExact, bool kF32>
+template <int kC, int kV, bool kExact, bool kF32>
 hipError_t launch_prefill_form(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, hipStream_t stream) {
     constexpr int kStageBlocks = kC <= 2 ? 2 : 1;
-    if (tile == PrefillTile::Rows64) return launch_prefill_tiles<kC, kExact, 1, kStageBlocks, 4, kC <= 4 ? 4 : 2, kF32>(a, parts, kv, stream);
-    return launch_prefill_tiles<kC, kExact, kC <= 4 ? 2 : 1, kStageBlocks, kC <= 4 ? 4 : 8, kC <= 4 && !kF32 ? 3 : 2, kF32>(a, parts, kv, stream);
+    if (tile == PrefillTile::Rows64) return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kC <= 4 ? 4 : 2, kF32>(a, parts, kv, stream);
+    return launch_prefill_tiles<kC, kV, kExact, kC <= 4 ? 2 : 1, kStageBlocks, kC <= 4 ? 4 : 8, kC <= 4 && !kF32 ? 3 : 2, kF32>(a, parts, kv, stream);
 }
 // compiled in translation units of their own
-template <int kC, bool kExact>
+template <int kC, int kV, bool kExact>
 hipError_t launch_prefill(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream) {
-    return f32 ? launch_prefill_form<kC, kExact, true>(tile, a, parts, kv, stream) : launch_prefill_form<kC, kExact, false>(tile, a, parts, kv, stream);
+    return f32 ? launch_prefill_form<kC, kV, kExact, true>(tile, a, parts, kv, stream) : launch_prefill_form<kC, kV, kExact, false>(tile, a, parts, kv, stream);
 }
 
 }  // namespace bitnet

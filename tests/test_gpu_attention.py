@@ -60,7 +60,7 @@ def check_attention(got, q, batch, rows, scale, f32, label=""):
         assert np.all(off <= bounds[1 if f32 else 0]), (label, t, b, pos, float(np.nanmax(off)), float((off / bounds[1 if f32 else 0]).max()), bool(np.isnan(off).any()))
 
 
-DIMS = [2, 8, 40, 64, 80, 100, 128, 160, 192, 250, 256]
+DIMS = [2, 8, 24, 40, 56, 64, 80, 90, 96, 100, 120, 128, 160, 192, 250, 256]
 
 
 # ---- rotary positions and the cache -----------------------------------------------------------------------------------------
