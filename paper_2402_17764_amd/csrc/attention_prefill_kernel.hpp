@@ -32,7 +32,11 @@ enum class PrefillTile { Rows64, Rows128 };
 constexpr int prefill_rows(PrefillTile t) { return t == PrefillTile::Rows64 ? 64 : 128; }
 constexpr float kSlack = 8.0f;         // in the exponent of 2
 
-constexpr int prefill_piece(int Dp) { return (Dp * 64 + 1023) / 1024 * 1024; }     // a block's keys (or values) in LDS: whole wave loads
+// LDS of a cache block: the keys' 4 kC quads of 512 bytes, then the values, 16 kV dims of each of the four groups of eight tokens.  Where a head has
+// fewer, its last eight dims of the same token, and a group's last dim, stand again, so that the groups are multiples of 256
+// bytes apart (in the cache's own steps of 16 Dp, heads of 100, reads met in LDS banks on 28 % of the cycles).  Queries have zeros
+// there, and results of such dims are not stored.
+constexpr int prefill_lds(int kC, int kV, int blocks) { return 2 * blocks * (2 * kC + kV) * 1024; }
 
 template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
 __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(PrefillArgs a, Parts parts, KvView kv) {
@@ -45,8 +49,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     char* lds = reinterpret_cast<char*>(smem);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
-    const int D = kExact ? 32 * kC : kv.D, Dp = kv_padded_dim(D), quads = Dp >> 3;
-    const int piece = kExact ? prefill_piece(32 * kC) : prefill_piece(Dp), stage_bytes = 2 * kStageBlocks * piece;
+    const int D = kExact ? 32 * kC : kv.D, Dp = kv_padded_dim(D);
+    constexpr int kKeyPiece = 2 * kC * 1024, kValuePiece = kV * 1024, kStage = kStageBlocks * (kKeyPiece + kValuePiece);
 
     // Heads side by side: with a multiple of eight of them a head's tiles meet on one XCD, whose L2 then holds its keys and values once.
     const int h = blockIdx.x % kv.kv_heads;
@@ -87,36 +91,31 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         numbers = blk < blocks ? kv.block(table, blk, h) : -1;
     };
     const int64_t block_bytes = (int64_t)kKvBlock * Dp * 2;
-    // 1 KiB at a time: the stage's key blocks, then its value blocks, dealt out to the waves.  What a block's padding to whole loads reaches
-    // behind the block's end comes back as zeros.
+    // 1 KiB at a time, the keys of the stage's blocks, then their values, dealt out to the waves
     auto copy = [&](int stage) {
-        constexpr int kLoads = 2 * kC, kAll = 2 * kStageBlocks * kLoads;
-        char* to = lds + (stage & 1) * stage_bytes;
+        constexpr int kKeyLoads = kStageBlocks * 2 * kC, kAll = kKeyLoads + kStageBlocks * kV;
+        char* to = lds + (stage & 1) * kStage;
 #pragma unroll
         for (int j = 0; j < (kAll + kW - 1) / kW; ++j) {
             const int p = j * kW + wave;
             if (kAll % kW && p >= kAll) break;
-            const int what = kLoads % kW == 0 ? j * kW / kLoads : p / kLoads, i = kLoads % kW == 0 ? j * kW % kLoads + wave : p % kLoads;
-            if (!kExact && i >= piece >> 10) continue;
-            const int64_t at = max(__builtin_amdgcn_readlane(numbers, (stage * kStageBlocks + what % kStageBlocks) & 63), 0) * block_bytes;
-            const __amdgpu_buffer_rsrc_t rsrc =
-                __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(what < kStageBlocks ? kv.k : kv.v) + at, 0, (int)block_bytes, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + what * piece + i * 1024), 16, i * 1024 + lane * 16, 0, 0, 0);
+            const bool key = kKeyLoads % kW == 0 ? j * kW < kKeyLoads : p < kKeyLoads;
+            const int at_kind = key ? p : p - kKeyLoads, of = key ? 2 * kC : kV, u = kStageBlocks == 1 ? 0 : at_kind / of, i = at_kind - u * of;
+            const int64_t at = max(__builtin_amdgcn_readlane(numbers, (stage * kStageBlocks + u) & 63), 0) * block_bytes;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(key ? kv.k : kv.v) + at, 0, (int)block_bytes, 0x00020000);
+            const int quad = i * 64 + lane;
+            const int from = kExact ? quad : key ? min(quad >> 5, (Dp >> 3) - 1) * 32 + (quad & 31) : quad / (16 * kV) * Dp + min(quad % (16 * kV), Dp - 1);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + p * 1024), 16, from * 16, 0, 0, 0);
         }
     };
-    int koff[kC], voff[kV];
-#pragma unroll
-    for (int c = 0; c < kC; ++c) koff[c] = (kExact || c < whole_chunks(kC) ? 4 * c + g : min(4 * c + g, quads - 1)) * 512 + r * 16;
-#pragma unroll
-    for (int i = 0; i < kV; ++i) voff[i] = (g * Dp + (kExact || i < 2 * whole_chunks(kC) ? 16 * i + r : min(16 * i + r, Dp - 1))) * 16;
+    const int koff = g * 512 + r * 16, voff = (g * (16 * kV) + r) * 16;
 
-    v4f acc[kNT][kV], l[kNT];                                              // l: the sum of the weights, four times
-    float m[kNT];
-    const v8bf ones = ones_operand();
+    v4f acc[kNT][kV];
+    float m[kNT], l[kNT];                                                  // l: of this lane's tokens
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         m[n] = kMinusInf;
-        l[n] = (v4f){0, 0, 0, 0};
+        l[n] = 0.0f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) acc[n][i] = (v4f){0, 0, 0, 0};
     }
@@ -125,16 +124,16 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     // A wave's matrix instructions run beside its exponentials where the source puts them so, a slice at a time with a fence behind each: the
     // scores of the second block with the weights of the first, the values of the first with the weights of the second.  Operands are read
     // from LDS kAhead fragments ahead of their products, keys and values in one sequence.
-    constexpr int kParts = kF32 ? 3 : 1, kAhead = 4, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
+    constexpr int kParts = kF32 ? 3 : 1, kAhead = 3, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
     auto take = [&](auto masked_, const char* keys, const char* values, int j0, const bool (&known)[kU]) {
         constexpr bool kMasked = decltype(masked_)::value;
         v4f sc[kU][2][kNT];
         v8bf w[kU][kNT][kParts], frag[kAhead];
         float base[kNT];
         auto read = [&](int f) {
-            if (f < kKeys * kU) frag[f % kAhead] = *reinterpret_cast<const v8bf*>(keys + f / kKeys * piece + koff[f / 2 % kC] + 256 * (f & 1));
+            if (f < kKeys * kU) frag[f % kAhead] = *reinterpret_cast<const v8bf*>(keys + f / kKeys * kKeyPiece + koff + 2048 * (f / 2 % kC) + 256 * (f & 1));
             else if (f < (kKeys + kV) * kU)
-                frag[f % kAhead] = *reinterpret_cast<const v8bf*>(values + (f - kKeys * kU) / kV * piece + voff[(f - kKeys * kU) % kV]);
+                frag[f % kAhead] = *reinterpret_cast<const v8bf*>(values + (f - kKeys * kU) / kV * kValuePiece + voff + 256 * ((f - kKeys * kU) % kV));
         };
         // the i-th of `slices` shares of block u's weights, two at a time
         auto weights = [&](int u, int i, int slices) {
@@ -143,6 +142,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 const int n = q / 4, j = q % 4 * 2;
                 const float p0 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][j & 3], a.scale, -base[n]));
                 const float p1 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][(j & 3) + 1], a.scale, -base[n]));
+                l[n] += p0;
+                l[n] += p1;
                 weights_pair<kF32>(w[u][n], j, p0, p1);
             }
         };
@@ -157,14 +158,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        auto sum = [&](int u) {
-#pragma unroll
-            for (int n = 0; n < kNT; ++n)
-#pragma unroll
-                for (int e = 0; e < kParts; ++e) l[n] = mfma_bf16(ones, w[u][n][e], l[n]);
-        };
         auto product = [&](int u, int with) {
-            sum(u);
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
                 const int f = kU * kKeys + u * kV + i;
@@ -197,10 +191,9 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
             }
             if (__builtin_amdgcn_ballot_w64(passed)) {
                 if (u > 0) {
-                    sum(u - 1);
 #pragma unroll
                     for (int i = 0; i < kV; ++i) {
-                        const v8bf v = *reinterpret_cast<const v8bf*>(values + (u - 1) * piece + voff[i]);
+                        const v8bf v = *reinterpret_cast<const v8bf*>(values + (u - 1) * kValuePiece + voff + 256 * i);
 #pragma unroll
                         for (int n = 0; n < kNT; ++n)
 #pragma unroll
@@ -254,10 +247,10 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     // are cleared in LDS, and of the others what is not finite, which is noted: rows that see it get NaN in its dim at the end, the rows in
     // front of it their sums.
     auto clean = [&](char* values, int j0, const bool (&known)[kStageBlocks]) {
-        for (int i = threadIdx.x; i < kStageBlocks * 4 * Dp; i += 64 * kW) {
-            const int u = i / (4 * Dp), at = i - u * 4 * Dp, first = j0 + u * kKvBlock + at / Dp * 8, d = at % Dp;
+        for (int i = threadIdx.x; i < kStageBlocks * 64 * kV; i += 64 * kW) {
+            const int u = i / (64 * kV), at = i % (64 * kV), first = j0 + u * kKvBlock + at / (16 * kV) * 8, d = at % (16 * kV);
             const int some = known[u] ? min(max(seen - first, 0), 8) : 0;
-            uint4* place = reinterpret_cast<uint4*>(values + u * piece + at * 16);
+            uint4* place = reinterpret_cast<uint4*>(values + i * 16);
             v4u v = __builtin_bit_cast(v4u, *place);
             values_keep(v, some);
             unsigned bad = 0;
@@ -280,8 +273,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         const int j0 = s * kStageBlocks * kKvBlock, at = (s * kStageBlocks) & 63;
         if (j0 + kStageBlocks * kKvBlock - 1 > tile_pos || __builtin_amdgcn_readlane(numbers, at) < 0 || __builtin_amdgcn_readlane(numbers, at + kStageBlocks - 1) < 0) break;
         stage_there(s);
-        const char* keys = lds + (s & 1) * stage_bytes;
-        const char* values = keys + kStageBlocks * piece;
+        const char* keys = lds + (s & 1) * kStage;
+        const char* values = keys + kStageBlocks * kKeyPiece;
         const bool known[kU] = {};
         take(std::false_type(), keys, values, j0, known);
     }
@@ -291,8 +284,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #pragma unroll
         for (int u = 0; u < kStageBlocks; ++u) known[u] = __builtin_amdgcn_readlane(numbers, (s * kStageBlocks + u) & 63) >= 0;
         stage_there(s);
-        char* keys = lds + (s & 1) * stage_bytes;
-        char* values = keys + kStageBlocks * piece;
+        char* keys = lds + (s & 1) * kStage;
+        char* values = keys + kStageBlocks * kKeyPiece;
         clean(values, j0, known);
         __syncthreads();
         if (j0 > pos_last) continue;                                       // nothing that this wave's rows see
@@ -300,7 +293,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
-        const float total = l[n][0], inv = total > 0.0f ? 1.0f / total : 0.0f;
+        const float total = groups_sum(l[n]), inv = total > 0.0f ? 1.0f / total : 0.0f;
         if (out_row[n] < 0) continue;
         const int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
         const bool whole = run >= all_stages;
@@ -326,13 +319,13 @@ template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kO
 hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView& kv, hipStream_t stream) {
     static RaisedFlags raised;
     const auto kernel = attention_prefill_tiles<kC, kV, kExact, kNT, kStageBlocks, kW, kOcc, kF32>;
-    const int lds = 2 * 2 * kStageBlocks * prefill_piece(kv_padded_dim(kv.D));
-    if (lds > 65536 - 2048) {                              // with the static part
-        const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(kernel), 2 * 2 * kStageBlocks * prefill_piece(32 * kC), raised);
+    constexpr int kLds = prefill_lds(kC, kV, kStageBlocks);
+    if (kLds > 65536 - 2048) {                             // with the static part
+        const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds, raised);
         if (e != hipSuccess) return e;
     }
     a.tiles = (int)tiles_at_most(a.T, kv.B, a.group, 16 * kNT * kW, 1);
-    kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, lds, stream>>>(a, parts, kv);
+    kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, kLds, stream>>>(a, parts, kv);
     return hipGetLastError();
 }
 template <int kC, int kV, bool kExact, bool kF32>
