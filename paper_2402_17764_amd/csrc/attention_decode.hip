@@ -201,7 +201,7 @@ hipError_t launch_decode(const DecodeArgs& a, const Parts& parts, const KvView& 
 // How many workgroups share a row at most, by the length that the page tables have room for.  A CU draws 25 to 45 bytes a cycle,
 // whatever number of waves asks, and a second launch costs 4 us in a chain of launches: so rows are shared where there are fewer
 // than 256 and more than 1023 tokens (one token, 32 heads of 128, a key-value head each, 1000 tokens: 13.4 us in one launch, 10.0 shared;
-// 500 tokens 8.6 / 9.4; 64 heads over 8, 1000 tokens 9.4 / 9.4), until there are two for each CU (three sequences of 23000 to 41000
+// 64 heads over 8, 500 tokens 7.5 / 9.5, 1000 tokens 9.4 / 9.4), until there are two for each CU (three sequences of 23000 to 41000
 // tokens, 64 heads over 8: 512 workgroups 74.7 us, 1024 79.1, 2048 79.2, none shared 359).  More rows are shared only at every
 // 8192 tokens, so that one long sequence among short ones is not what the call waits for.
 struct Splits { int n, least; };
