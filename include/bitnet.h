@@ -506,6 +506,8 @@ bitnet_status bitnet_unpack_weights(const void* packed, int64_t N, int64_t K, bi
  *   sequences        their number B
  *   page_table       [B] rows of max_pages int32 (device), table_stride elements apart: the page of position pos of sequence b is
  *                    page_table[b*table_stride + pos/page_tokens].  Entries behind a sequence's length are not used.
+ *                    max_pages bounds the lengths, and workgroups are allotted by it: a wide table's first columns alone, as many as the
+ *                    longest sequence needs, serve short sequences faster.
  *   kv_len           [B] int32 (device): tokens of the sequence, those of the call included.  Lengths outside 0 ... max_pages*page_tokens
  *                    count as the nearest of the two.
  *   q_start          [B+1] int32 (device), not falling: rows q_start[b] .. q_start[b+1]-1 of the call are the last tokens of sequence b, so
@@ -539,7 +541,7 @@ bitnet_status bitnet_kv_cache_bytes(int64_t pages, int64_t page_tokens, int64_t 
  *   rotary_dims   the first dims of a head, even, 0 ... head_dim: turned; the others pass unturned.  pairs == 0: dim i goes with dim
  *             i + rotary_dims/2; otherwise 2i with 2i+1.  (a, b) -> (a cos - b sin, b cos + a sin), in fp32
  *   T         rows of qkv; == kv->sequences if kv->q_start is NULL (BITNET_ERR_SHAPE otherwise)
- *   q         out [T][heads][head_dim] BF16, 2-byte aligned; bf16 (round to nearest even) as the cache is
+ *   q         out [T][heads][head_dim] BF16, 2-byte aligned, not overlapping qkv; bf16 (round to nearest even) as the cache is
  * One launch.
  */
 bitnet_status bitnet_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, const float* inv_freq, int64_t rotary_dims, int pairs,
@@ -547,10 +549,11 @@ bitnet_status bitnet_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, con
 
 /*
  * o = softmax(scale q . k) v over the cached keys and values of each row's sequence; query head i reads key-value head i / (heads/kv_heads).
- * The row at position pos sees the keys of positions 0 .. pos, whatever memory holds behind them.  Scores, weights' sums and the
+ * The row at position pos sees the keys of positions 0 .. pos, whatever memory holds behind them: what is not finite there, or in values of
+ * later positions, reaches no row that does not see it.  Scores, weights' sums and the
  * sums over values are fp32; weights enter their product as bf16, for an F32 result as the sum of two bf16.
  *   q          [rows][heads][head_dim] BF16, 2-byte aligned, as bitnet_rope_kv_append writes it
- *   scale      > 0 and finite (BITNET_ERR_SHAPE otherwise), ordinarily 1/sqrt(head_dim)
+ *   scale      > 0 and finite (BITNET_ERR_SHAPE otherwise), ordinarily 1/sqrt(head_dim); scores times scale have to be finite fp32 as well
  *   o          out [rows][heads*head_dim], F32 or BF16, element-aligned: what bitnet_quantize_acts or bitnet_linear_fused takes next
  *   workspace  device memory, 16-byte aligned, or NULL: contents are scratch; calls that share it must not overlap.  With the
  *              bitnet_attention_workspace() bytes or more, few rows on long sequences are spread over the chip: parts of a sequence are

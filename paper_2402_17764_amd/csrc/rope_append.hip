@@ -76,23 +76,23 @@ __device__ inline uint4 pack8(const float (&x)[8]) {
 }
 
 // A slot: dims d0 ... d0 + 7 of a head with what they are turned with, requested before any of it is used.  Dims that are turned across a
-// multiple of eight have partners in both directions.  Reads reach up to seven elements behind a head of queries or keys,
-// where the row goes on: values follow.
+// multiple of eight have partners in both directions.  Reads may reach behind a head, to the row's end and not further.
 enum class Turned { Split, Pairs, Any };
 template <bool kBf16, Turned kTurned>
 struct Slot {
     Eight<kBf16> own, low, high;       // low: partners of the dims of the lower half; Split: those alone
-    __device__ void load(const void* base, int64_t head, int d0, int D, bool turned, const RopeShape& s) {
+    // head: the head's first element among all, left: elements from there to the row's end
+    __device__ void load(const void* base, int64_t head, int64_t left, int d0, int D, bool turned, const RopeShape& s) {
         own = load8<kBf16>(base, head + d0, D - d0);
         const int half = s.rotary >> 1;
         if (kTurned == Turned::Split) {
             if (d0 < half) low = load8<kBf16>(base, head + d0 + half, 8);
         } else if (kTurned == Turned::Any && turned && d0 < s.rotary) {
-            if (d0 < half) low = load8<kBf16>(base, head + d0 + half, 8);
+            if (d0 < half) low = load8<kBf16>(base, head + d0 + half, (int)min(left - d0 - half, (int64_t)8));
             if (d0 + 8 > half) {
                 // in front of the tensor there is nothing: eight elements from its first one on, moved up
                 const int64_t at = head + d0 - half;
-                high = load8<kBf16>(base, at < 0 ? 0 : at, 8);
+                high = load8<kBf16>(base, at < 0 ? 0 : at, (int)min(head + left - (at < 0 ? 0 : at), (int64_t)8));
                 if (at < 0) {
                     using E = std::conditional_t<kBf16, uint16_t, uint32_t>;
                     E u[8], v[8];
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_tokens(const void* __res
     const int pos = kv.length(kv.kv_len[b]) - 1;
     const bool turned = mine && unit < s.heads + kv.kv_heads;
     Slot<kBf16, Turned::Any> slot;
-    if (mine) slot.load(qkv, head, d0, D, turned && !s.pairs, s);
+    if (mine) slot.load(qkv, head, (int64_t)(units - unit) * D, d0, D, turned && !s.pairs, s);
     for (int i = threadIdx.x; i < s.rotary >> 1; i += kThreads) turns[i] = turn_of(pos, inv_freq[i]);
     __syncthreads();
     float x[8], none[8];
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
     auto request = [&](Slot<kBf16, kTurned> (&x)[kM], int u) {
 #pragma unroll
         for (int m = 0; m < kM; ++m)
-            if (tok[m] >= 0) x[m].load(qkv, ((int64_t)(row0 + tok[m]) * units + u) * D, d0[m], D, u < s.heads + kv.kv_heads, s);
+            if (tok[m] >= 0) x[m].load(qkv, ((int64_t)(row0 + tok[m]) * units + u) * D, (int64_t)(units - u) * D, d0[m], D, u < s.heads + kv.kv_heads, s);
     };
     request(next, u0);
 #pragma unroll 1
