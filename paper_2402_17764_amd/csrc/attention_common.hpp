@@ -11,7 +11,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
 // The sizes of heads that the kernels are built for: kC chunks of 32 dims for the scores, kV tiles of 16 for the values.  Exact: all of them are
-// whole.  Otherwise the last may be filled in part -- kWhole chunks are not -- and up to 128 dims the last chunk has one tile or two.
+// whole.  Otherwise whole_chunks(kC) are, those behind may be filled in part, and up to 128 dims the last chunk has one tile or two.
 constexpr int whole_chunks(int kC) { return kC <= 4 ? kC - 1 : kC - 2; }
 
 constexpr float kMinusInf = -__builtin_inff();
@@ -149,7 +149,8 @@ struct JoinArgs {
 };
 hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream);
 
-// The prefill kernel's tile of a sequence's rows for one head: the keys that its last token sees, in stages of 64 tokens.
+// The prefill kernel's tile of a sequence's rows for one head: the keys that its last token sees, and how many 64 tokens of them (the unit in
+// which they are shared out).
 constexpr int kStageTokens = 64;
 __device__ inline int tile_sees(const NewTokens& nt, int64_t row_last, int group) { return nt.pos0 + (int)(row_last / group) + 1; }
 __device__ inline int stages_of(int seen) { return seen > 0 ? (seen + kStageTokens - 1) / kStageTokens : 0; }

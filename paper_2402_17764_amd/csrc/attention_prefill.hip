@@ -25,7 +25,7 @@ static PrefillPlan prefill_plan(const KvView& kv, int64_t T, int heads) {
     const bool behind_others = capacity >= 4 * (T / kv.B);
     if (rows_a_sequence >= 1024 && large >= (behind_others ? 512 : 1024)) return {PrefillTile::Rows128, 1, 1};
     const int64_t small = tiles_at_most(T, kv.B, group, 64, 1) * kv.kv_heads, n = capacity >= 1024 ? 512 / small : 1;
-    constexpr int kLeast = 4;                              // stages of 64 tokens
+    constexpr int kLeast = 4;                              // times 64 tokens
     int64_t most = ceil_div(capacity, kLeast * kStageTokens);
     most = most < kMostSplits ? most : kMostSplits;
     return {PrefillTile::Rows64, (int)(n < 2 ? 1 : n < most ? n : most), kLeast};
@@ -37,7 +37,8 @@ size_t attention_prefill_workspace_bytes(const KvView& kv, int64_t T, int heads)
 
 hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, void* workspace,
                                     size_t workspace_bytes, hipStream_t stream) {
-    const PrefillArgs a{static_cast<const uint16_t*>(q), o, scale * 1.44269504f, heads, heads / kv.kv_heads, (int)T, 0};
+    const float by = scale * 1.44269504f;
+    const PrefillArgs a{static_cast<const uint16_t*>(q), o, by, fminf(kSlack / by, 3e38f), heads, heads / kv.kv_heads, (int)T, 0};
     const PrefillPlan plan = prefill_plan(kv, T, heads);
     Parts parts;
     if (plan.splits > 1 && workspace_bytes >= Parts::bytes(T * heads, plan.splits, kv.D)) parts = Parts(workspace, T * heads, plan.splits, plan.least, kv.D);

@@ -3,9 +3,9 @@
 // with the running maximum and sum of a softmax in 32 bits, one pass over the keys.
 //
 // A workgroup takes a tile of rows of one sequence and one key-value head -- a row is one query head of one new token, the heads of a
-// group next to each other, so that grouped heads share what they read -- and walks the cache 64 tokens at a time.  Both cache
-// blocks come through LDS (copied as they stand, by loads that go to LDS directly; the cache's order is already that of the MFMA
-// operands), double-buffered: the next blocks are requested right behind the barrier that publishes the current ones.  Scores are products
+// group next to each other, so that grouped heads share what they read -- and walks the cache a stage of one or two blocks
+// of 32 tokens at a time.  Keys and values come through LDS (copied as they stand, by loads that go to LDS directly; the cache's order is
+// already that of the MFMA operands), double-buffered: the next stage is requested right behind the barrier that publishes the current one.  Scores are products
 // keys (down) times queries (across), which leaves a lane with eight consecutive tokens of its query: the operand of the second product.
 #pragma once
 #include "attention_common.hpp"
@@ -18,6 +18,7 @@ struct PrefillArgs {
     const uint16_t* q;
     void* o;
     float scale;                       // of the softmax, times log2 e
+    float slack;                       // kSlack in units of a score; finite, so that the first score of all passes
     int heads, group, T;               // query heads, and of them per key-value head; rows of q
     int tiles;                         // of the launch, per key-value head
 };
@@ -111,25 +112,25 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     const int koff = g * 512 + r * 16, voff = (g * (16 * kV) + r) * 16;
 
     v4f acc[kNT][kV];
-    float m[kNT], l[kNT];                                                  // l: of this lane's tokens
+    float m[kNT], base[kNT], l[kNT];                                       // base: m times scale, or 0; l: of this lane's tokens
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         m[n] = kMinusInf;
-        l[n] = 0.0f;
+        base[n] = l[n] = 0.0f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) acc[n][i] = (v4f){0, 0, 0, 0};
     }
     // A stage's blocks, in LDS from `keys` and `values` on, the first token at position j0.  Masked: some row does not see all of them.
     //
-    // A wave's matrix instructions run beside its exponentials where the source puts them so, a slice at a time with a fence behind each: the
-    // scores of the second block with the weights of the first, the values of the first with the weights of the second.  Operands are read
-    // from LDS kAhead fragments ahead of their products, keys and values in one sequence.
+    // A wave's matrix instructions run beside its exponentials where the source puts them so, a slice at a time with a fence behind each: in a
+    // stage of two blocks the scores of the second with the weights of the first, the values of the first with the weights of the second (with
+    // one block, the other waves' matrix instructions fill that time).  Operands are read from LDS kAhead fragments ahead of their products,
+    // keys and values in one sequence.
     constexpr int kParts = kF32 ? 3 : 1, kAhead = 3, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
     auto take = [&](auto masked_, const char* keys, const char* values, int j0, const bool (&known)[kU]) {
         constexpr bool kMasked = decltype(masked_)::value;
         v4f sc[kU][2][kNT];
         v8bf w[kU][kNT][kParts], frag[kAhead];
-        float base[kNT];
         auto read = [&](int f) {
             if (f < kKeys * kU) frag[f % kAhead] = *reinterpret_cast<const v8bf*>(keys + f / kKeys * kKeyPiece + koff + 2048 * (f / 2 % kC) + 256 * (f & 1));
             else if (f < (kKeys + kV) * kU)
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #pragma unroll
                 for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[u][j >> 2][n][j & 3]);
                 tops[n] = top;
-                passed = passed || top * a.scale > m[n] * a.scale + kSlack;
+                passed = passed || top > m[n] + a.slack;
             }
             if (__builtin_amdgcn_ballot_w64(passed)) {
                 if (u > 0) {
@@ -205,6 +206,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 for (int n = 0; n < kNT; ++n) {
                     const float now = fmaxf(m[n], groups_max(tops[n])), by = now == kMinusInf ? 1.0f : exp2_fast((m[n] - now) * a.scale);
                     m[n] = now;
+                    base[n] = now == kMinusInf ? 0.0f : now * a.scale;
                     l[n] *= by;
 #pragma unroll
                     for (int i = 0; i < kV; ++i) acc[n][i] *= by;
@@ -213,8 +215,6 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                         for (int e = 0; e < kParts; ++e) w[u - 1][n][e] = v8bf{};
                 }
             }
-#pragma unroll
-            for (int n = 0; n < kNT; ++n) base[n] = m[n] == kMinusInf ? 0.0f : m[n] * a.scale;
             __builtin_amdgcn_sched_barrier(0);
         };
 #pragma unroll
