@@ -75,18 +75,21 @@ __device__ inline uint4 pack8(const float (&x)[8]) {
     return __builtin_bit_cast(uint4, w);
 }
 
-// A slot: dims d0 ... d0 + 7 of a head with what they are turned with, requested before any of it is used.  Dims that are turned across a
-// multiple of eight have partners in both directions.  Reads may reach behind a head, to the row's end and not further.
-enum class Turned { Split, Pairs, Any };
+// A slot: dims d0 ... d0 + 7 of a head with what they are turned with, requested before any of it is used.  Split and Odd: slots of the lower
+// half are turned together with their partners, whose slots there are none of; Odd is for halves that are no multiple of eight
+// (of a half's last slot some dims may be the other half's and are not used).  Any: slots of all dims, each turned alone; such
+// as cross the middle have partners in both directions.  Reads may reach behind a head, to the row's end and not further.
+enum class Turned { Split, Odd, Pairs, Any };
 template <bool kBf16, Turned kTurned>
 struct Slot {
-    Eight<kBf16> own, low, high;       // low: partners of the dims of the lower half; Split: those alone
+    static constexpr bool kTogether = kTurned == Turned::Split || kTurned == Turned::Odd;
+    Eight<kBf16> own, low, high;       // low: partners of the dims of the lower half; Split, Odd: those alone
     // head: the head's first element among all, left: elements from there to the row's end
     __device__ void load(const void* base, int64_t head, int64_t left, int d0, int D, bool turned, const RopeShape& s) {
-        own = load8<kBf16>(base, head + d0, D - d0);
+        own = load8<kBf16>(base, head + d0, kTurned == Turned::Odd ? (int)min(left - d0, (int64_t)8) : D - d0);
         const int half = s.rotary >> 1;
-        if (kTurned == Turned::Split) {
-            if (d0 < half) low = load8<kBf16>(base, head + d0 + half, 8);
+        if (kTogether) {
+            if (d0 < half) low = load8<kBf16>(base, head + d0 + half, kTurned == Turned::Odd ? (int)min(left - d0 - half, (int64_t)8) : 8);
         } else if (kTurned == Turned::Any && turned && d0 < s.rotary) {
             if (d0 < half) low = load8<kBf16>(base, head + d0 + half, (int)min(left - d0 - half, (int64_t)8));
             if (d0 + 8 > half) {
@@ -108,11 +111,11 @@ struct Slot {
             }
         }
     }
-    // x: own dims turned; y (Split): the partners, turned
+    // x: own dims turned; y (Split, Odd): the partners, turned
     __device__ void turn(float (&x)[8], float (&y)[8], int d0, bool turned, const Turn (&t)[8], const RopeShape& s) const {
         floats_of<kBf16>(x, own);
         const int half = s.rotary >> 1;
-        if (kTurned == Turned::Split) {
+        if (kTogether) {
             if (d0 < half) floats_of<kBf16>(y, low);
             if (!turned || d0 >= half) return;
 #pragma unroll
@@ -144,6 +147,21 @@ struct Slot {
 };
 
 __device__ inline int pair_of(int d, const RopeShape& s) { return s.pairs ? d >> 1 : d < (s.rotary >> 1) ? d : d - (s.rotary >> 1); }
+
+// n of eight elements into LDS, two at a time where p allows it
+__device__ inline void stage_any(uint16_t* p, uint4 w, int n, bool words) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    if (words) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (2 * i + 1 < n) *reinterpret_cast<uint32_t*>(p + 2 * i) = u[i];
+        if (n & 1)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) if (i + 1 == n) p[i] = (uint16_t)u[i >> 1];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < n) p[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+}
 
 __device__ inline void store_any(uint16_t* p, uint4 w, int count) {
     if (count >= 8) { __builtin_memcpy(p, &w, 16); return; }
@@ -201,17 +219,26 @@ __global__ __launch_bounds__(kThreads) void rope_append_tokens(const void* __res
     }
 }
 
+// The slots of a head: those of the lower half, and those of the dims that are not turned.
+template <Turned kTurned>
+constexpr int slots_of(int D, const RopeShape& s) {
+    if (kTurned == Turned::Pairs) return (D + 7) / 8;
+    return (s.rotary / 2 + 7) / 8 + (D - s.rotary + 7) / 8;
+}
+
 // Runs of new tokens: a workgroup takes the new tokens of one cache block (32 positions) and `per` heads of their rows.  A thread keeps
 // its token and dims over the heads, so that sines and cosines are computed once and stay in registers.  Values are turned
 // over through LDS: the cache holds eight tokens of a dim together.
 //
-// What a thread takes of a head is a slot: eight dims, or where the halves that are turned together begin at multiples of eight (Split)
-// eight of the lower half and their eight partners, each of which is read once.
+// What a thread takes of a head is a slot: eight dims, or where halves are turned together eight of the lower half and their eight partners,
+// so that each is read and each angle computed once.  Where the halves do not begin at multiples of eight (Odd) the results
+// come together in LDS first, as the cache takes eight dims at a time (4096 tokens, 32 heads of 100: 52 us, where slots of all
+// dims read their partners on both sides 83; 32 heads of 40, fp32: 29.6, there 28.2).
 template <bool kBf16, Turned kTurned, int kM /* slots a thread */>
 __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, KvView kv,
                                                                RopeShape s, int per, uint16_t* __restrict__ q) {
     constexpr int kPitch = 256 + 8;
-    __shared__ uint4 tile4[kTurned == Turned::Any ? kKvBlock * 128 / 2 : kKvBlock * kPitch / 8];      // Any: sines and cosines first
+    __shared__ uint4 tile4[kKvBlock * kPitch / 8];
     uint16_t* tile = reinterpret_cast<uint16_t*>(tile4);
     const int D = kv.D, Dp = kv_padded_dim(D), quads = Dp >> 3, units = s.heads + 2 * kv.kv_heads;
     const int b = sequence_of_tile(kv.q_start, kv.B, blockIdx.x, 1, kKvBlock, 2);
@@ -227,8 +254,9 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
     // the page: its number is the same for all heads
     const int page_index = blk >= 0 ? blk / kv.page_blocks : 0, page = blk >= 0 ? kv.table[b * kv.table_stride + page_index] : -1;
 
-    const int half8 = s.rotary >> 4;                           // Split: quads of a half
-    const int slots = kTurned == Turned::Split ? quads - half8 : quads, tiles = (slots + 7) >> 3;
+    constexpr bool kTogether = kTurned == Turned::Split || kTurned == Turned::Odd;
+    const int half = s.rotary >> 1, half8 = (half + 7) >> 3;   // slots of a half
+    const int slots = slots_of<kTurned>(D, s), tiles = (slots + 7) >> 3;
     int tok[kM], d0[kM];
     Turn turn[kM][8];
 #pragma unroll
@@ -237,27 +265,18 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
         const int i = threadIdx.x + m * kThreads, j = (i & 7) + 8 * ((i >> 6) % tiles);
         tok[m] = ((i >> 3) & 7) + 8 * ((i >> 6) / tiles);
         if (j >= slots || tok[m] < t0 || tok[m] >= t1) tok[m] = -1;
-        // Split: the lower half's quads, then those that are not turned
-        d0[m] = 8 * (kTurned == Turned::Split && j >= half8 ? j + half8 : j);
-        if (kTurned != Turned::Any && tok[m] >= 0 && u0 < s.heads + kv.kv_heads)
+        // the lower half's, then those that are not turned
+        d0[m] = kTogether && j >= half8 ? s.rotary + 8 * (j - half8) : 8 * j;
+        if (tok[m] >= 0 && u0 < s.heads + kv.kv_heads)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (kTurned == Turned::Pairs && (e & 1)) { turn[m][e] = turn[m][e - 1]; continue; }
-                turn[m][e] = d0[m] + e < s.rotary ? turn_of(blk * kKvBlock + tok[m], inv_freq[pair_of(d0[m] + e, s)]) : Turn{1.0f, 0.0f};
+                const bool angle = kTurned == Turned::Odd ? d0[m] + e < half : d0[m] + e < s.rotary;
+                turn[m][e] = angle ? turn_of(blk * kKvBlock + tok[m], inv_freq[pair_of(d0[m] + e, s)]) : Turn{1.0f, 0.0f};
             }
     }
-    if (kTurned == Turned::Any && u0 < s.heads + kv.kv_heads) {      // two dims have an angle: computed once, taken twice
-        Turn* table = reinterpret_cast<Turn*>(tile4);
-        const int half = s.rotary >> 1;
-        for (int i = threadIdx.x; i < kKvBlock * half; i += kThreads) table[i] = turn_of(blk * kKvBlock + i / half, inv_freq[i % half]);
-        __syncthreads();
-#pragma unroll
-        for (int m = 0; m < kM; ++m)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (tok[m] >= 0 && d0[m] + e < s.rotary) turn[m][e] = table[tok[m] * half + pair_of(d0[m] + e, s)];
-        __syncthreads();
-    }
+    if (kTurned == Turned::Odd)                                // dims behind a head's end
+        for (int i = threadIdx.x; i < kKvBlock * (Dp - D); i += kThreads) tile[i / (Dp - D) * kPitch + D + i % (Dp - D)] = 0;
     Slot<kBf16, kTurned> slot[kM], next[kM];
     auto request = [&](Slot<kBf16, kTurned> (&x)[kM], int u) {
 #pragma unroll
@@ -280,17 +299,31 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
             if (tok[m] < 0) continue;
             const int64_t out = ((int64_t)(row0 + tok[m]) * s.heads + u) * D;
             auto put = [&](int d, uint4 w) {
-                if (query) store_any(q + out + d, w, D - d);
+                if (kTurned == Turned::Odd) stage_any(&tile[tok[m] * kPitch + d], w, d0[m] < half ? min(half - d0[m], 8) : min(D - d0[m], 8), (half & 1) == 0 || d == d0[m]);
+                else if (query) store_any(q + out + d, w, D - d);
                 else if (key) *reinterpret_cast<uint4*>(kv.k + at + kv_key_at(tok[m], d)) = w;
                 else *reinterpret_cast<uint4*>(&tile[tok[m] * kPitch + d]) = w;
             };
             float x[8], y[8];
             slot[m].turn(x, y, d0[m], query || key, turn[m], s);
             put(d0[m], pack8(x));
-            if (kTurned == Turned::Split && d0[m] < 8 * half8) put(d0[m] + 8 * half8, pack8(y));
+            if (kTogether && d0[m] < half) put(d0[m] + half, pack8(y));
         }
-        if (query || key) continue;
+        if (kTurned != Turned::Odd && (query || key)) continue;
         __syncthreads();
+        if (query || key) {
+            // queries by rows, as in memory; keys by eight dims of 32 tokens, which stand next to each other in the cache
+            const int across = query ? (quads + 7) >> 3 : 0;
+            for (int i = threadIdx.x; i < 32 * (query ? 8 * across : quads); i += kThreads) {
+                const int j = query ? (i & 7) + 8 * ((i >> 6) % across) : i >> 5, t = query ? ((i >> 3) & 7) + 8 * ((i >> 6) / across) : i & 31;
+                if (j >= quads || t < t0 || t >= t1) continue;
+                const uint4 w = *reinterpret_cast<const uint4*>(&tile[t * kPitch + 8 * j]);
+                if (query) store_any(q + ((int64_t)(row0 + t) * s.heads + u) * D + 8 * j, w, D - 8 * j);
+                else *reinterpret_cast<uint4*>(kv.k + at + kv_key_at(t, 8 * j)) = w;
+            }
+            __syncthreads();
+            continue;
+        }
         for (int i = threadIdx.x; i < 4 * D; i += kThreads) {
             const int g = i / D, d = i - g * D;
             if (8 * g + 8 <= t0 || 8 * g >= t1) continue;
@@ -313,8 +346,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
 
 template <bool kBf16, Turned kTurned>
 hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& kv, const RopeShape& s, uint16_t* q, hipStream_t stream) {
-    const int units = s.heads + 2 * kv.kv_heads, quads = kv_padded_dim(kv.D) / 8;
-    const int slots = kTurned == Turned::Split ? quads - (s.rotary >> 4) : quads, m = (slots + 7) / 8;
+    const int units = s.heads + 2 * kv.kv_heads, m = (slots_of<kTurned>(kv.D, s) + 7) / 8;
     const int64_t tiles = tiles_at_most(s.T, kv.B, 1, kKvBlock, 2);
     // Heads of a workgroup: four share a token's sines and cosines and the loads that say where its row and its page are, if that leaves
     // three workgroups for each CU, and fewer otherwise (us, one / two / four / eight: 4096 tokens, 64 heads over 8, two prompts 65 /
@@ -324,14 +356,15 @@ hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& k
     const dim3 grid((unsigned)tiles, (unsigned)ceil_div(units, per));
     if (m == 1) rope_append_blocks<kBf16, kTurned, 1><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
     else if (m == 2) rope_append_blocks<kBf16, kTurned, 2><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
-    else rope_append_blocks<kBf16, kTurned, 4><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
+    else if (kTurned != Turned::Odd || m <= 4) rope_append_blocks<kBf16, kTurned, 4><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
+    else rope_append_blocks<kBf16, Turned::Odd, 5><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);      // 33 slots
     return hipGetLastError();
 }
 template <bool kBf16>
 hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& kv, const RopeShape& s, uint16_t* q, hipStream_t stream) {
     if (s.pairs) return launch_blocks<kBf16, Turned::Pairs>(qkv, inv_freq, kv, s, q, stream);
     if (s.rotary % 16 == 0) return launch_blocks<kBf16, Turned::Split>(qkv, inv_freq, kv, s, q, stream);
-    return launch_blocks<kBf16, Turned::Any>(qkv, inv_freq, kv, s, q, stream);
+    return launch_blocks<kBf16, Turned::Odd>(qkv, inv_freq, kv, s, q, stream);
 }
 
 }  // namespace

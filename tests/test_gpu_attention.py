@@ -129,7 +129,7 @@ def test_append_runs(gpu_lib, D, pairs):
 
 
 @pytest.mark.parametrize("one", [False, True])
-@pytest.mark.parametrize("rotary,D", [(0, 64), (2, 64), (32, 128), (24, 100), (98, 100)])
+@pytest.mark.parametrize("rotary,D", [(0, 64), (2, 64), (32, 128), (24, 100), (98, 100), (2, 256), (2, 250), (14, 90), (240, 250)])
 def test_append_turns_the_first_dims_alone(gpu_lib, one, rotary, D):
     sizes = [(3, 1), (70, 1)] if one else [(3, 40), (70, 1)]
     for pairs in (False, True):
@@ -214,21 +214,21 @@ def test_decode_leaves_out_pages_that_are_not_there(gpu_lib):
 
 
 # ---- runs of tokens ----------------------------------------------------------------------------------------------------------
-def run_prefill(gpu_lib, sizes, heads, kv_heads, D, P, f32, seed=0, first=0, behind=0, per=None, rows=None, workspace=None):
+def run_prefill(gpu_lib, sizes, heads, kv_heads, D, P, f32, seed=0, first=0, behind=0, per=None, rows=None, workspace=None, scale=None, std=1.5):
     lens = [o + n for o, n in sizes]
     batch = Batch([max(n, 0) for n in lens], P, kv_heads, D, seed, per)
     T = first + sum(n for _, n in sizes) + behind
-    q = batch.queries(T, heads, D)
+    q = batch.queries(T, heads, D, std)
     start = np.cumsum([first] + [n for _, n in sizes])
     y = torch.full((T, heads * D), 7.25, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
-    got = gpu_lib.attention_prefill(dev16(q), batch.k, batch.v, dev(batch.table), dev(lens), dev(start), None, gpu_lib.F32 if f32 else gpu_lib.BF16, y=y,
+    got = gpu_lib.attention_prefill(dev16(q), batch.k, batch.v, dev(batch.table), dev(lens), dev(start), scale, gpu_lib.F32 if f32 else gpu_lib.BF16, y=y,
                                     workspace=workspace)
     assert got is y
     at = [(b, o + i) for b, (o, n) in enumerate(sizes) for i in range(n)]
     got = host(y)
     assert np.all(got[:first] == 7.25) and np.all(got[T - behind:] == 7.25)
     picked = range(len(at)) if rows is None else sorted({0, len(at) - 1} | set(int(i) for i in batch.rng.integers(0, len(at), rows)))
-    check_attention(got[[first + i for i in picked]], q[[first + i for i in picked]], batch, [at[i] for i in picked], D ** -0.5, f32, "D %d" % D)
+    check_attention(got[[first + i for i in picked]], q[[first + i for i in picked]], batch, [at[i] for i in picked], scale or D ** -0.5, f32, "D %d" % D)
 
 
 @pytest.mark.parametrize("D", DIMS)
@@ -261,6 +261,15 @@ def test_prefill_long_runs(gpu_lib, D, sizes):
 @pytest.mark.parametrize("sizes", [[(3000, 5)], [(2000, 20), (0, 3), (255, 1), (256, 1)], [(1500, 0), (1040, 70)], [(-2, 4), (1100, 2)]])
 def test_prefill_shared_rows(gpu_lib, D, sizes):
     run_prefill(gpu_lib, sizes, 6, 2, D, 32, D != 128, seed=5, first=1, behind=2)
+
+
+# weights from all alike (scores that no float of the exponent's size tells apart) to one alone
+@pytest.mark.parametrize("scale,std", [(1e-39, 1.0), (1e-30, 1.0), (1e-3, 1.0), (0.7, 0.0), (1.0, 3.0), (20.0, 4.0)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_peaked_and_flat_weights(gpu_lib, D, scale, std):
+    run_prefill(gpu_lib, [(0, 300), (45, 1)], 4, 2, D, 64, True, seed=6, rows=40, scale=scale, std=std)
+    run_prefill(gpu_lib, [(3000, 5)], 4, 2, D, 64, False, seed=6, scale=scale, std=std)
+    run_decode(gpu_lib, [4000, 45], 4, 2, D, 64, True, seed=6, scale=scale, std=std)
 
 
 def test_prefill_values_that_are_not_finite_stay_with_the_rows_that_see_them(gpu_lib):
