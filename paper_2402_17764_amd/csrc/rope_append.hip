@@ -86,7 +86,7 @@ struct Slot {
     Eight<kBf16> own, low, high;       // low: partners of the dims of the lower half; Split, Odd: those alone
     // head: the head's first element among all, left: elements from there to the row's end
     __device__ void load(const void* base, int64_t head, int64_t left, int d0, int D, bool turned, const RopeShape& s) {
-        own = load8<kBf16>(base, head + d0, kTurned == Turned::Odd ? (int)min(left - d0, (int64_t)8) : D - d0);
+        own = load8<kBf16>(base, head + d0, kTurned == Turned::Odd || kTurned == Turned::Pairs ? (int)min(left - d0, (int64_t)8) : D - d0);
         const int half = s.rotary >> 1;
         if (kTogether) {
             if (d0 < half) low = load8<kBf16>(base, head + d0 + half, kTurned == Turned::Odd ? (int)min(left - d0 - half, (int64_t)8) : 8);
@@ -163,11 +163,14 @@ __device__ inline void stage_any(uint16_t* p, uint4 w, int n, bool words) {
     for (int i = 0; i < 8; ++i) if (i < n) p[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
 }
 
+// A head's last dims, `count` even: what stands behind them cleared, or left out.  (A last slot that is read past its head and written in one or
+// two pieces, as against element by element: 4096 tokens, 32 heads of 100, pairs 55 -> 48 us.)
+__device__ inline uint4 first_of(uint4 w, int count) { return {w.x, count > 2 ? w.y : 0, count > 4 ? w.z : 0, count > 6 ? w.w : 0}; }
 __device__ inline void store_any(uint16_t* p, uint4 w, int count) {
     if (count >= 8) { __builtin_memcpy(p, &w, 16); return; }
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 7; ++i) if (i < count) p[i] = (uint16_t)(u[i >> 1] >> (16 * (i & 1)));
+    if (count & 4) __builtin_memcpy(p, &w, 8);
+    const uint32_t two = count & 4 ? w.z : w.x;
+    if (count & 2) __builtin_memcpy(p + (count & 4), &two, 4);
 }
 
 // One new token for each sequence.  A thread takes eight dims of a head; what counts is the chain of loads (length, page, row),
@@ -232,7 +235,7 @@ constexpr int slots_of(int D, const RopeShape& s) {
 //
 // What a thread takes of a head is a slot: eight dims, or where halves are turned together eight of the lower half and their eight partners,
 // so that each is read and each angle computed once.  Where the halves do not begin at multiples of eight (Odd) the results
-// come together in LDS first, as the cache takes eight dims at a time (4096 tokens, 32 heads of 100: 52 us, where slots of all
+// come together in LDS first, as the cache takes eight dims at a time (4096 tokens, 32 heads of 100: 48 us, where slots of all
 // dims read their partners on both sides 83; 32 heads of 40, fp32: 29.6, there 28.2).
 template <bool kBf16, Turned kTurned, int kM /* slots a thread */>
 __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, KvView kv,
@@ -301,7 +304,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
             auto put = [&](int d, uint4 w) {
                 if (kTurned == Turned::Odd) stage_any(&tile[tok[m] * kPitch + d], w, d0[m] < half ? min(half - d0[m], 8) : min(D - d0[m], 8), (half & 1) == 0 || d == d0[m]);
                 else if (query) store_any(q + out + d, w, D - d);
-                else if (key) *reinterpret_cast<uint4*>(kv.k + at + kv_key_at(tok[m], d)) = w;
+                else if (key) *reinterpret_cast<uint4*>(kv.k + at + kv_key_at(tok[m], d)) = kTurned == Turned::Pairs ? first_of(w, D - d) : w;
                 else *reinterpret_cast<uint4*>(&tile[tok[m] * kPitch + d]) = w;
             };
             float x[8], y[8];
