@@ -59,14 +59,27 @@ __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
         const int d0 = 32 * c + 8 * g;
-        uint16_t u[8] = {};
+        v4u w = {0, 0, 0, 0};
         if (row) {
-            if (d0 + 8 <= D) __builtin_memcpy(u, row + d0, 16);
-            else
+            if (c < whole_chunks(kC) || D == 32 * kC) {
+                __builtin_memcpy(&w, row + d0, 16);
+            } else if (D >= 8) {                           // the last eight dims, moved to their places: one load, whatever is left
+                const int over = max(d0 + 8 - D, 0) >> 1;
+                __builtin_memcpy(&w, row + min(d0, D - 8), 16);
+                if (over & 1) w = (v4u){w[1], w[2], w[3], 0};
+                if (over & 2) w = (v4u){w[2], w[3], 0, 0};
+                if (over >= 4) w = (v4u){0, 0, 0, 0};
+            } else {
 #pragma unroll
-                for (int i = 0; i < 7; ++i) if (d0 + i < D) u[i] = row[d0 + i];
+                for (int i = 0; i < 3; ++i)
+                    if (d0 + 2 * i < D) {
+                        uint32_t two;
+                        __builtin_memcpy(&two, row + d0 + 2 * i, 4);
+                        w[i] = two;
+                    }
+            }
         }
-        __builtin_memcpy(&f[c], u, 16);
+        f[c] = __builtin_bit_cast(v8bf, w);
     }
 }
 
