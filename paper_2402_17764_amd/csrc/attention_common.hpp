@@ -53,7 +53,7 @@ __device__ inline float exp2_fast(float x) {
 }
 
 // A query row's operand: dims 32 c + 8 g ... + 7 (zeros behind the head's end, so that what lies behind the keys' dims counts
-// for nothing).  `row` NULL: no such query.
+// for nothing -- once settle_query is through).  `row` NULL: no such query.
 template <int kC>
 __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int D) {
 #pragma unroll
@@ -63,12 +63,8 @@ __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int
         if (row) {
             if (c < whole_chunks(kC) || D == 32 * kC) {
                 __builtin_memcpy(&w, row + d0, 16);
-            } else if (D >= 8) {                           // the last eight dims, moved to their places: one load, whatever is left
-                const int over = max(d0 + 8 - D, 0) >> 1;
+            } else if (D >= 8) {                           // the last eight dims: one load, whatever is left
                 __builtin_memcpy(&w, row + min(d0, D - 8), 16);
-                if (over & 1) w = (v4u){w[1], w[2], w[3], 0};
-                if (over & 2) w = (v4u){w[2], w[3], 0, 0};
-                if (over >= 4) w = (v4u){0, 0, 0, 0};
             } else {
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
@@ -79,6 +75,22 @@ __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int
                     }
             }
         }
+        f[c] = __builtin_bit_cast(v8bf, w);
+    }
+}
+
+// The last dims that load_query read, to their places.  A call of its own, as it waits for them: other loads go out in between (one prompt
+// of 64 tokens and 32 heads of 126: 0.5 us).
+template <int kC>
+__device__ inline void settle_query(v8bf (&f)[kC], int g, int D) {
+    if (D == 32 * kC || D < 8) return;
+#pragma unroll
+    for (int c = whole_chunks(kC); c < kC; ++c) {
+        const int over = max(32 * c + 8 * g + 8 - D, 0) >> 1;
+        v4u w = __builtin_bit_cast(v4u, f[c]);
+        if (over & 1) w = (v4u){w[1], w[2], w[3], 0};
+        if (over & 2) w = (v4u){w[2], w[3], 0, 0};
+        if (over >= 4) w = (v4u){0, 0, 0, 0};
         f[c] = __builtin_bit_cast(v8bf, w);
     }
 }
@@ -165,7 +177,8 @@ hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const Kv
 // The prefill kernel's tile of a sequence's rows for one head: the keys that its last token sees, and how many 64 tokens of them (the unit in
 // which they are shared out).
 constexpr int kStageTokens = 64;
-__device__ inline int tile_sees(const NewTokens& nt, int64_t row_last, int group) { return nt.pos0 + (int)(row_last / group) + 1; }
+__device__ inline int token_of(int row, int group) { return (int)((unsigned)row / (unsigned)group); }
+__device__ inline int tile_sees(const NewTokens& nt, int row_last, int group) { return nt.pos0 + token_of(row_last, group) + 1; }
 __device__ inline int stages_of(int seen) { return seen > 0 ? (seen + kStageTokens - 1) / kStageTokens : 0; }
 
 __device__ inline int blocks_of(const KvView& kv, int b) { return (kv.length(kv.kv_len[b]) + kKvBlock - 1) / kKvBlock; }

@@ -28,8 +28,9 @@ __device__ inline int splits_of(const JoinArgs& a, const Parts& parts, const KvV
         const int b = sequence_of_tile(kv.q_start, kv.B, t, 1, 1, 0);
         const NewTokens nt(kv, b, a.T);
         if (t < nt.first || t >= nt.first + nt.n) return 0;
-        const int64_t rows = (int64_t)nt.n * a.group, row = (int64_t)(t - nt.first) * a.group + head % a.group, tile = row / a.rows_a_tile;
-        units = stages_of(tile_sees(nt, min((tile + 1) * a.rows_a_tile, rows) - 1, a.group));
+        const int row = (t - nt.first) * a.group + head % a.group;
+        const int behind = (row / a.rows_a_tile + 1) * a.rows_a_tile;
+        units = stages_of(tile_sees(nt, min(behind, nt.n * a.group) - 1, a.group));
     }
     const int run = parts.run(units);
     return (units + run - 1) / run;

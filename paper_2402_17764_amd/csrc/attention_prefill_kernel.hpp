@@ -58,11 +58,11 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     const int64_t x = a.tiles - 1 - (int)(blockIdx.x / kv.kv_heads);       // late tiles, which see most, first
     const int b = sequence_of_tile(kv.q_start, kv.B, x, a.group, kRows, 1);
     const NewTokens nt(kv, b, a.T);
+    // tokens times heads are below 2^28, so rows have 32 bits: 64-bit quotients are a hundred instructions each in front of the first load
     const int64_t tile = x - first_tile(kv.q_start[b], b, a.group, kRows, 1);
-    const int64_t rows = (int64_t)nt.n * a.group;
-    if (tile < 0 || tile * kRows >= rows) return;
-    const int64_t row0 = tile * kRows;                                     // of the sequence's rows for this head
-    const int64_t row_last = min(row0 + kRows, rows) - 1;
+    const int rows = nt.n * a.group, row0 = (int)tile * kRows;             // of the sequence, for this head
+    if (tile < 0 || row0 >= rows) return;
+    const int row_last = min(row0 + kRows, rows) - 1;
     const int seen = tile_sees(nt, row_last, a.group);                     // keys that the tile's last token sees
     const int blocks = seen > 0 ? (seen + kKvBlock - 1) / kKvBlock : 0, all_stages = stages_of(seen);
     // this workgroup's stages
@@ -73,17 +73,16 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     v8bf qf[kNT][kC];
     int pos[kNT];                                                          // of the lane's queries; -1: none
     int out_row[kNT];                                                      // row of q times heads, plus head; -1: none
-    const int64_t wave_row = row0 + wave * 16 * kNT;
+    const int wave_row = row0 + wave * 16 * kNT;
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
-        const int64_t R = wave_row + 16 * n + r;
-        const int tok = (int)(R / a.group), hh = (int)(R - (int64_t)tok * a.group);
+        const int R = wave_row + 16 * n + r, tok = token_of(R, a.group), hh = R - tok * a.group;
         out_row[n] = R < rows ? (nt.first + tok) * a.heads + h * a.group + hh : -1;
         pos[n] = R < rows ? nt.pos0 + tok : -1;
         load_query<kC>(qf[n], R < rows ? a.q + (int64_t)out_row[n] * D : nullptr, g, D);
     }
-    const int tile_pos = nt.pos0 + (int)(row0 / a.group);                  // of the tile's first token, and of the wave's last
-    const int pos_last = wave_row < rows ? nt.pos0 + (int)((min(wave_row + 16 * kNT, rows) - 1) / a.group) : -1;
+    const int tile_pos = nt.pos0 + token_of(row0, a.group);                 // of the tile's first token, and of the wave's last
+    const int pos_last = wave_row < rows ? nt.pos0 + token_of(min(wave_row + 16 * kNT, rows) - 1, a.group) : -1;
 
     const int32_t* table = kv.table + b * kv.table_stride;
     int numbers = -1;                                                      // of 64 blocks, one a lane
@@ -243,6 +242,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         fetch_numbers((stage0 * kStageBlocks) & ~63);
         copy(stage0);
     }
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) settle_query<kC>(qf[n], g, D);
     // The values of a stage that some row does not see to its end.  A weight of zero does not make an infinity nothing: tokens that no row sees
     // are cleared in LDS, and of the others what is not finite, which is noted: rows that see it get NaN in its dim at the end, the rows in
     // front of it their sums.
