@@ -52,6 +52,14 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     const int r = lane & 15, g = lane >> 4;
     const int D = kExact ? 32 * kC : kv.D, Dp = kv_padded_dim(D);
     constexpr int kKeyPiece = 2 * kC * 1024, kValuePiece = kV * 1024, kStage = kStageBlocks * (kKeyPiece + kValuePiece);
+    // where this lane's share of a wave's pieces of a stage comes from, bytes within a block
+    constexpr int kKeyLoads = kStageBlocks * 2 * kC, kAll = kKeyLoads + kStageBlocks * kV, kPieces = (kAll + kW - 1) / kW;
+    int piece_from[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        const int p = j * kW + wave, key = p % (2 * kC) * 64 + lane, value = (p - kKeyLoads) % kV * 64 + lane;
+        piece_from[j] = 16 * (p < kKeyLoads ? min(key >> 5, (Dp >> 3) - 1) * 32 + (key & 31) : value / (16 * kV) * Dp + min(value % (16 * kV), Dp - 1));
+    }
 
     // Heads side by side: with a multiple of eight of them a head's tiles meet on one XCD, whose L2 then holds its keys and values once.
     const int h = blockIdx.x % kv.kv_heads;
@@ -93,19 +101,17 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     const int64_t block_bytes = (int64_t)kKvBlock * Dp * 2;
     // 1 KiB at a time, the keys of the stage's blocks, then their values, dealt out to the waves
     auto copy = [&](int stage) {
-        constexpr int kKeyLoads = kStageBlocks * 2 * kC, kAll = kKeyLoads + kStageBlocks * kV;
         char* to = lds + (stage & 1) * kStage;
 #pragma unroll
-        for (int j = 0; j < (kAll + kW - 1) / kW; ++j) {
+        for (int j = 0; j < kPieces; ++j) {
             const int p = j * kW + wave;
             if (kAll % kW && p >= kAll) break;
             const bool key = kKeyLoads % kW == 0 ? j * kW < kKeyLoads : p < kKeyLoads;
             const int at_kind = key ? p : p - kKeyLoads, of = key ? 2 * kC : kV, u = kStageBlocks == 1 ? 0 : at_kind / of, i = at_kind - u * of;
             const int64_t at = max(__builtin_amdgcn_readlane(numbers, (stage * kStageBlocks + u) & 63), 0) * block_bytes;
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(key ? kv.k : kv.v) + at, 0, (int)block_bytes, 0x00020000);
-            const int quad = i * 64 + lane;
-            const int from = kExact ? quad : key ? min(quad >> 5, (Dp >> 3) - 1) * 32 + (quad & 31) : quad / (16 * kV) * Dp + min(quad % (16 * kV), Dp - 1);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + p * 1024), 16, from * 16, 0, 0, 0);
+            const int from = kExact ? (i * 64 + lane) * 16 : piece_from[j];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(to + p * 1024), 16, from, 0, 0, 0);
         }
     };
     const int koff = g * 512 + r * 16, voff = (g * (16 * kV) + r) * 16;
