@@ -5,8 +5,9 @@
 // A workgroup takes a tile of rows of one sequence and one key-value head -- a row is one query head of one new token, the heads of a
 // group next to each other, so that grouped heads share what they read -- and walks the cache a stage of one or two blocks
 // of 32 tokens at a time.  Keys and values come through LDS (copied as they stand, by loads that go to LDS directly; the cache's order is
-// already that of the MFMA operands), double-buffered: the next stage is requested right behind the barrier that publishes the current one.  Scores are products
-// keys (down) times queries (across), which leaves a lane with eight consecutive tokens of its query: the operand of the second product.
+// already that of the MFMA operands), double-buffered: the next stage is requested right behind the barrier that publishes the current
+// one.  Scores are products keys (down) times queries (across), which leaves a lane with eight consecutive tokens of its query: the
+// operand of the second product.
 #pragma once
 #include "attention_common.hpp"
 
@@ -68,8 +69,9 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     const NewTokens nt(kv, b, a.T);
     // tokens times heads are below 2^28, so rows have 32 bits: 64-bit quotients are a hundred instructions each in front of the first load
     const int64_t tile = x - first_tile(kv.q_start[b], b, a.group, kRows, 1);
-    const int rows = nt.n * a.group, row0 = (int)tile * kRows;             // of the sequence, for this head
-    if (tile < 0 || row0 >= rows) return;
+    const int rows = nt.n * a.group;                                       // of the sequence, for this head
+    if (tile < 0 || tile * kRows >= rows) return;
+    const int row0 = (int)tile * kRows;
     const int row_last = min(row0 + kRows, rows) - 1;
     const int seen = tile_sees(nt, row_last, a.group);                     // keys that the tile's last token sees
     const int blocks = seen > 0 ? (seen + kKvBlock - 1) / kKvBlock : 0, all_stages = stages_of(seen);
