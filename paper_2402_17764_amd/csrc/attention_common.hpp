@@ -54,16 +54,16 @@ __device__ inline float exp2_fast(float x) {
 
 // A query row's operand: dims 32 c + 8 g ... + 7 (zeros behind the head's end, so that what lies behind the keys' dims counts
 // for nothing -- once settle_query is through).  `row` NULL: no such query.
-template <int kC>
+template <int kC, bool kExact>
 __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int D) {
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
         const int d0 = 32 * c + 8 * g;
         v4u w = {0, 0, 0, 0};
         if (row) {
-            if (c < whole_chunks(kC) || D == 32 * kC) {
+            if (kExact || c < whole_chunks(kC)) {
                 __builtin_memcpy(&w, row + d0, 16);
-            } else if (D >= 8) {                           // the last eight dims: one load, whatever is left
+            } else if (kC > 1 || D >= 8) {                 // the last eight dims: one load, whatever is left
                 __builtin_memcpy(&w, row + min(d0, D - 8), 16);
             } else {
 #pragma unroll
@@ -81,9 +81,9 @@ __device__ inline void load_query(v8bf (&f)[kC], const uint16_t* row, int g, int
 
 // The last dims that load_query read, to their places.  A call of its own, as it waits for them: other loads go out in between (one prompt
 // of 64 tokens and 32 heads of 126: 0.5 us).
-template <int kC>
+template <int kC, bool kExact>
 __device__ inline void settle_query(v8bf (&f)[kC], int g, int D) {
-    if (D == 32 * kC || D < 8) return;
+    if (kExact || (kC == 1 && D < 8)) return;
 #pragma unroll
     for (int c = whole_chunks(kC); c < kC; ++c) {
         const int over = max(32 * c + 8 * g + 8 - D, 0) >> 1;

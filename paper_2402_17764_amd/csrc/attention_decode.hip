@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
     if (blk0 >= blocks && blockIdx.y > 0) return;
 
     v8bf qf[kC];
-    load_query<kC>(qf, r < columns ? a.q + ((int64_t)b * a.heads + head0 + r) * D : nullptr, g, D);
+    load_query<kC, kExact>(qf, r < columns ? a.q + ((int64_t)b * a.heads + head0 + r) * D : nullptr, g, D);
 
     int koff[kC], voff[kV];                                // bytes within a block
 #pragma unroll
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
         fetch_numbers(0);
         load(x0, 0);
     }
-    settle_query<kC>(qf, g, D);
+    settle_query<kC, kExact>(qf, g, D);
     for (int it = 0; it < mine; it += 2) {                 // two sets of registers that swap roles by name
         const bool known0 = __builtin_amdgcn_readlane(numbers, it & 63) >= 0;
         bool known1 = false;

@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         const int R = wave_row + 16 * n + r, tok = token_of(R, a.group), hh = R - tok * a.group;
         out_row[n] = R < rows ? (nt.first + tok) * a.heads + h * a.group + hh : -1;
         pos[n] = R < rows ? nt.pos0 + tok : -1;
-        load_query<kC>(qf[n], R < rows ? a.q + (int64_t)out_row[n] * D : nullptr, g, D);
+        load_query<kC, kExact>(qf[n], R < rows ? a.q + (int64_t)out_row[n] * D : nullptr, g, D);
     }
     const int tile_pos = nt.pos0 + token_of(row0, a.group);                 // of the tile's first token, and of the wave's last
     const int pos_last = wave_row < rows ? nt.pos0 + token_of(min(wave_row + 16 * kNT, rows) - 1, a.group) : -1;
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         copy(stage0);
     }
 #pragma unroll
-    for (int n = 0; n < kNT; ++n) settle_query<kC>(qf[n], g, D);
+    for (int n = 0; n < kNT; ++n) settle_query<kC, kExact>(qf[n], g, D);
     // The values of a stage that some row does not see to its end.  A weight of zero does not make an infinity nothing: tokens that no row sees
     // are cleared in LDS, and of the others what is not finite, which is noted: rows that see it get NaN in its dim at the end, the rows in
     // front of it their sums.
@@ -308,13 +308,13 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         const bool whole = run >= all_stages;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int d = 16 * i + 4 * g;
-            if (d >= D) continue;
+            const int d = 16 * i + 4 * g, end = kExact || i < 2 * whole_chunks(kC) ? d + 4 : D;
+            if (d >= end) continue;
             float out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[e] = pos[n] >= bad_at[d + e] ? __builtin_nanf("") : whole ? acc[n][i][e] * inv : acc[n][i][e];
-            if (whole) store4<kF32>(a.o, (int64_t)out_row[n] * D, d, D, out);
-            else store4<true>(parts.sums, place * D, d, D, out);
+            if (whole) store4<kF32>(a.o, (int64_t)out_row[n] * D, d, end, out);
+            else store4<true>(parts.sums, place * D, d, end, out);
         }
         if (!whole && g == 0) {
             parts.state[2 * place] = m[n];
