@@ -95,19 +95,21 @@ __device__ inline void settle_query(v8bf (&f)[kC], int g, int D) {
     }
 }
 
-// Weights as operands, the pair j, j + 1 of eight.  bf16 keeps 8 bits of each: the sums of products then carry a relative error of about
-// 2^-9 / sqrt(keys), which a bf16 result hides.  For a 32-bit result what that rounding leaves goes through the product too, and what its
-// rounding leaves: three operands hold all 24 bits of a weight (two leave 2^-17 of it: measured 1.3e-6 of the result, three 2e-7).
-template <bool kF32>
+// Weights as operands, the pair j, j + 1 of eight, in kParts bf16 each: what the rounding of one leaves goes through the product too.  One keeps 8
+// bits of a weight, which puts an error of the size of a bf16 result's own rounding on it; two leave 2^-17 of a weight, which such a
+// result hides; three hold all 24 bits, for a 32-bit result (measured 1.3e-6 of the result with two, 2e-7 with three).  What they
+// cost is a product of values each: of single tokens, which wait for memory, next to nothing (us, one / two / three: 29 sequences of up to 4096
+// tokens, 32 heads of 128 160 / 164 / 162, 64 heads over 8, 20000 to 49000 tokens 73.6 / 74.2 / 74.5, 1000 tokens 8.4 / 8.6 / 8.8), of
+// runs a quarter of the time or more (40 heads of 128, 2048 tokens 57 / 73, 64 heads over 8, 1024 behind 15000 445 / 666).  So
+// decode takes two for a bf16 result and prefill one, and both take three for fp32.
+template <int kParts>
 __device__ inline void weights_pair(v8bf* w, int j, float p0, float p1) {
-    w[0][j] = (__bf16)p0;
-    w[0][j + 1] = (__bf16)p1;
-    if (kF32) {
-        const float r0 = p0 - (float)w[0][j], r1 = p1 - (float)w[0][j + 1];
-        w[1][j] = (__bf16)r0;
-        w[1][j + 1] = (__bf16)r1;
-        w[2][j] = (__bf16)(r0 - (float)w[1][j]);
-        w[2][j + 1] = (__bf16)(r1 - (float)w[1][j + 1]);
+#pragma unroll
+    for (int e = 0; e < kParts; ++e) {
+        w[e][j] = (__bf16)p0;
+        w[e][j + 1] = (__bf16)p1;
+        p0 -= (float)w[e][j];
+        p1 -= (float)w[e][j + 1];
     }
 }
 

@@ -24,7 +24,7 @@ struct DecodeArgs {
 // parts.splits workgroups (blockIdx.y).
 template <int kC, int kV, bool kExact, bool kF32, int kW>
 __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_rows(DecodeArgs a, Parts parts, KvView kv) {
-    constexpr int kWholeChunks = whole_chunks(kC);
+    constexpr int kWholeChunks = whole_chunks(kC), kParts = kF32 ? 3 : 2;      // bf16 operands of a weight
     constexpr int kRound = kV < 4 ? kV : 4;                // tiles that the waves add up at a time
     constexpr int kPitch = 16 * kRound + 4;
     __shared__ float sums[kW * 16 * kPitch], maxima[kW * 16], totals[kW * 16];
@@ -107,13 +107,13 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
         const float base = m == kMinusInf ? 0.0f : m * a.scale;
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = exp2_fast(__builtin_fmaf(p[j], a.scale, -base));
-        v8bf w[kF32 ? 3 : 1];
+        v8bf w[kParts];
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) weights_pair<kF32>(w, j, p[j], p[j + 1]);
+        for (int j = 0; j < 8; j += 2) weights_pair<kParts>(w, j, p[j], p[j + 1]);
 #pragma unroll
-        for (int e = 0; e < (kF32 ? 3 : 1); ++e) l = mfma_bf16(ones, w[e], l);
+        for (int e = 0; e < kParts; ++e) l = mfma_bf16(ones, w[e], l);
 #pragma unroll
-        for (int e = 0; e < (kF32 ? 3 : 1); ++e)
+        for (int e = 0; e < kParts; ++e)
 #pragma unroll
             for (int i = 0; i < kV; ++i) acc[i] = mfma_bf16(__builtin_bit_cast(v8bf, x.v[i]), w[e], acc[i]);
     };

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 const int n = q / 4, j = q % 4 * 2;
                 const float p0 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][j & 3], a.scale, -base[n]));
                 const float p1 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][(j & 3) + 1], a.scale, -base[n]));
-                weights_pair<kF32>(w[u][n], j, p0, p1);
+                weights_pair<kParts>(w[u][n], j, p0, p1);
                 l[n] = kF32 ? l[n] + p0 + p1 : add_rounded(l[n], w[u][n][0], j);
             }
         };

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from attention_ref import BF16_HALF_STEP, attention
 from test_gpu_attention import Batch, dev, dev16, host
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +34,20 @@ def test_values_all_alike_come_back(gpu_lib, sizes, heads, kv_heads, D, f32):
     for got in (y, one):
         off = np.abs(host(got).reshape(-1, kv_heads, heads // kv_heads, D) / c[:, None, :] - 1)
         assert off.max() <= ((2 * n + 64) * 2.0 ** -24 if f32 else 0.0), off.max()
+
+
+# one launch (up to three rounds of blocks, a sequence of no tokens), rows that workgroups share
+@pytest.mark.parametrize("lens", [[1, 2, 31, 33, 64, 0, 127, 129, 300], [5000], [4097, 1, 2050]])
+@pytest.mark.parametrize("D", [2, 24, 64, 100, 128, 160, 256])
+def test_decode_rounds_a_bf16_result_once(gpu_lib, lens, D):
+    """Weights of two bf16 operands leave 2^-17 of each, in the sums and in the divisor, which the bound of attention_ref for fp32 results
+    (2^-16, its scores and sums) has room for; the result's own half step comes on top and nothing of a weight's half step."""
+    heads, kv_heads = 6, 2
+    batch = Batch(lens, 96, kv_heads, D, 32)
+    q = batch.queries(len(lens), heads, D)
+    y = host(gpu_lib.attention_decode(dev16(q), batch.k, batch.v, dev(batch.table), dev(lens), y_dtype=gpu_lib.BF16))
+    for b, n in enumerate(lens):
+        k, v, there = batch.cache.get(batch.table[b], n)
+        o, (_, once) = attention(q[b], k, v, there, D ** -0.5)
+        off = np.abs(y[b].reshape(heads, D) - o)
+        assert (off <= once + BF16_HALF_STEP * (np.abs(o) + once)).all(), (n, (off / (once + BF16_HALF_STEP * np.abs(o))).max())
