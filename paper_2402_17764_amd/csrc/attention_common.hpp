@@ -142,6 +142,10 @@ __device__ inline void values_keep(v4u& v, int count) {
     for (int w = 0; w < 4; ++w) v[w] &= count >= 2 * w + 2 ? 0xFFFFFFFFu : count == 2 * w + 1 ? 0x0000FFFFu : 0u;
 }
 
+// A sum over values times `by`: NaN where the sum is an infinity.  An infinite value that a row sees meets weights of zero and factors of zero (0 inf) in some
+// tiles, splits and types and in others not, and what is noted of it where a tile ends (prefill) is NaN: so all of them say NaN.
+__device__ inline float finite_or_nan(float sum, float by) { return __builtin_fmaf(sum, 0.0f, sum * by); }
+
 // four consecutive outputs of a row of D, from dim d on
 template <bool kF32>
 __device__ inline void store4(void* o, int64_t at, int d, int D, const float (&x)[4]) {

@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
             }
             if (run >= blocks) {
                 const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-                const float out[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+                const float out[4] = {finite_or_nan(x[0], inv), finite_or_nan(x[1], inv), finite_or_nan(x[2], inv), finite_or_nan(x[3], inv)};
                 store4<kF32>(a.o, ((int64_t)b * a.heads + head0 + col) * D, dim, D, out);
             } else {
                 const float out[4] = {x[0], x[1], x[2], x[3]};

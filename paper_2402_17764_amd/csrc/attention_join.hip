@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void attention_join(JoinArgs a, Parts parts, K
     if (wave != 0 || dim >= D) return;
     x = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
     const float total = (totals[0] + totals[1]) + (totals[2] + totals[3]), inv = total > 0.0f ? 1.0f / total : 0.0f;
-    const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    const float y[4] = {finite_or_nan(x[0], inv), finite_or_nan(x[1], inv), finite_or_nan(x[2], inv), finite_or_nan(x[3], inv)};
     store4<kF32>(a.o, (int64_t)blockIdx.x * D, dim, D, y);
 }
 

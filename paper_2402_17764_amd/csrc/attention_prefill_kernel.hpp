@@ -305,13 +305,14 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         if (out_row[n] < 0) continue;
         const int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
         const bool whole = run >= all_stages;
+        const float by = whole ? inv : 1.0f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             const int d = 16 * i + 4 * g, end = kExact || i < 2 * whole_chunks(kC) ? d + 4 : D;
             if (d >= end) continue;
             float out[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = pos[n] >= bad_at[d + e] ? __builtin_nanf("") : whole ? acc[n][i][e] * inv : acc[n][i][e];
+            for (int e = 0; e < 4; ++e) out[e] = pos[n] >= bad_at[d + e] ? __builtin_nanf("") : finite_or_nan(acc[n][i][e], by);
             if (whole) store4<kF32>(a.o, (int64_t)out_row[n] * D, d, end, out);
             else store4<true>(parts.sums, place * D, d, end, out);
         }
