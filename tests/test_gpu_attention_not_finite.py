@@ -32,7 +32,7 @@ def check(got, want, heads, kv_heads, D, positions, first):
 # rows that workgroups share, tiles of 128 rows
 @pytest.mark.parametrize("old,new,heads,kv_heads,marks", [
     (0, 300, 4, 2, {40: INF}), (0, 300, 4, 2, {299: -INF}), (0, 300, 4, 2, {0: NAN}), (33, 130, 6, 2, {5: -INF, 64: INF}), (33, 130, 6, 2, {63: INF, 64: INF}),
-    (0, 1, 4, 2, {0: INF}), (3000, 5, 4, 2, {2999: INF}), (3000, 5, 4, 2, {7: -INF}), (3000, 5, 4, 2, {3002: INF}), (2100, 1030, 64, 8, {9: INF}), (2100, 1030, 64, 8, {2500: -INF})])
+    (0, 1, 4, 2, {0: INF}), (3000, 5, 4, 2, {2999: INF}), (3000, 5, 4, 2, {7: -INF}), (3000, 5, 4, 2, {3002: INF}), (3200, 1030, 64, 8, {9: INF}), (3200, 1030, 64, 8, {3600: -INF})])
 @pytest.mark.parametrize("D", [24, 64, 100, 128, 192])
 @pytest.mark.parametrize("f32", [False, True])
 def test_prefill(gpu_lib, old, new, heads, kv_heads, marks, D, f32):
