@@ -352,9 +352,11 @@ hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& k
     const int units = s.heads + 2 * kv.kv_heads, m = (slots_of<kTurned>(kv.D, s) + 7) / 8;
     const int64_t tiles = tiles_at_most(s.T, kv.B, 1, kKvBlock, 2);
     // Heads of a workgroup: four share a token's sines and cosines and the loads that say where its row and its page are, if that leaves
-    // three workgroups for each CU, and fewer otherwise (us, one / two / four / eight: 4096 tokens, 64 heads over 8, two prompts 65 /
-    // 49 / 40 / 41; 512 tokens 10.8 / 9.0 / 10.2 / 15.3; 77 tokens 5.2 / 5.5 / 6.8 / 11.2).
-    const int64_t all = tiles * units / 768;
+    // 704 workgroups, two and three quarters for each CU, of those that `tiles` counts (up to two a sequence have no token), and fewer
+    // otherwise (us, one / two / three / four: 64 heads over 8, two prompts of 2048 tokens 65 / 48 / 43 / 43, one of 2048 23 / 18.6 / 18.1 /
+    // 17.6, two of 512 14.7 / 12.6 / 12.7 / 12.7, one of 512 10.3 / 9.2 / 9.4 / 10.6, two of 256 10.0 / 9.6 / 10.1 / 10.7, one of 256 6.2 / 6.8 /
+    // 7.1 / 7.4, of 77 5.1 / 5.5 / 6.3 / 7.0; with 768 the one of 512 has one).
+    const int64_t all = tiles * units / 704;
     const int per = (int)(all < 1 ? 1 : all > 4 ? 4 : all);
     const dim3 grid((unsigned)tiles, (unsigned)ceil_div(units, per));
     if (m == 1) rope_append_blocks<kBf16, kTurned, 1><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
