@@ -222,10 +222,10 @@ __global__ __launch_bounds__(kThreads) void rope_append_tokens(const void* __res
     }
 }
 
-// The slots of a head: those of the lower half, and those of the dims that are not turned.
+// The slots of a head: those of the lower half, and those of the dims that are not turned; or all.
 template <Turned kTurned>
 constexpr int slots_of(int D, const RopeShape& s) {
-    if (kTurned == Turned::Pairs) return (D + 7) / 8;
+    if (kTurned == Turned::Pairs || kTurned == Turned::Any) return (D + 7) / 8;
     return (s.rotary / 2 + 7) / 8 + (D - s.rotary + 7) / 8;
 }
 
@@ -235,8 +235,8 @@ constexpr int slots_of(int D, const RopeShape& s) {
 //
 // What a thread takes of a head is a slot: eight dims, or where halves are turned together eight of the lower half and their eight partners,
 // so that each is read and each angle computed once.  Where the halves do not begin at multiples of eight (Odd) the results
-// come together in LDS first, as the cache takes eight dims at a time (4096 tokens, 32 heads of 100: 48 us, where slots of all
-// dims read their partners on both sides 83; 32 heads of 40, fp32: 29.6, there 28.2).
+// come together in LDS first, as the cache takes eight dims at a time, or slots of all dims read their partners on both sides (Any); see
+// launch_blocks.
 template <bool kBf16, Turned kTurned, int kM /* slots a thread */>
 __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, KvView kv,
                                                                RopeShape s, int per, uint16_t* __restrict__ q) {
@@ -270,13 +270,24 @@ __global__ __launch_bounds__(kThreads) void rope_append_blocks(const void* __res
         if (j >= slots || tok[m] < t0 || tok[m] >= t1) tok[m] = -1;
         // the lower half's, then those that are not turned
         d0[m] = kTogether && j >= half8 ? s.rotary + 8 * (j - half8) : 8 * j;
-        if (tok[m] >= 0 && u0 < s.heads + kv.kv_heads)
+        if (kTurned != Turned::Any && tok[m] >= 0 && u0 < s.heads + kv.kv_heads)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if (kTurned == Turned::Pairs && (e & 1)) { turn[m][e] = turn[m][e - 1]; continue; }
                 const bool angle = kTurned == Turned::Odd ? d0[m] + e < half : d0[m] + e < s.rotary;
                 turn[m][e] = angle ? turn_of(blk * kKvBlock + tok[m], inv_freq[pair_of(d0[m] + e, s)]) : Turn{1.0f, 0.0f};
             }
+    }
+    if (kTurned == Turned::Any && u0 < s.heads + kv.kv_heads) {      // two dims have an angle: computed once, taken twice
+        Turn* table = reinterpret_cast<Turn*>(tile4);          // [32][half]: heads of up to 64 dims
+        for (int i = threadIdx.x; i < kKvBlock * half; i += kThreads) table[i] = turn_of(blk * kKvBlock + i / half, inv_freq[i % half]);
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < kM; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (tok[m] >= 0 && d0[m] + e < s.rotary) turn[m][e] = table[tok[m] * half + pair_of(d0[m] + e, s)];
+        __syncthreads();
     }
     if (kTurned == Turned::Odd)                                // dims behind a head's end
         for (int i = threadIdx.x; i < kKvBlock * (Dp - D); i += kThreads) tile[i / (Dp - D) * kPitch + D + i % (Dp - D)] = 0;
@@ -360,6 +371,7 @@ hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& k
     const int per = (int)(all < 1 ? 1 : all > 4 ? 4 : all);
     const dim3 grid((unsigned)tiles, (unsigned)ceil_div(units, per));
     if (m == 1) rope_append_blocks<kBf16, kTurned, 1><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
+    else if constexpr (kTurned == Turned::Any) return hipErrorInvalidValue;
     else if (m == 2) rope_append_blocks<kBf16, kTurned, 2><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
     else if (kTurned != Turned::Odd || m <= 4) rope_append_blocks<kBf16, kTurned, 4><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);
     else rope_append_blocks<kBf16, Turned::Odd, 5><<<grid, kThreads, 0, stream>>>(qkv, inv_freq, kv, s, per, q);      // 33 slots
@@ -369,6 +381,11 @@ template <bool kBf16>
 hipError_t launch_blocks(const void* qkv, const float* inv_freq, const KvView& kv, const RopeShape& s, uint16_t* q, hipStream_t stream) {
     if (s.pairs) return launch_blocks<kBf16, Turned::Pairs>(qkv, inv_freq, kv, s, q, stream);
     if (s.rotary % 16 == 0) return launch_blocks<kBf16, Turned::Split>(qkv, inv_freq, kv, s, q, stream);
+    // Halves that are no multiple of eight: turned together through LDS, whose barriers cost more than partners that are read on both sides
+    // where a thread's one slot of eight is enough for that, a head of up to 64 dims (us, Odd / Any, 32 heads, 4096 tokens: of 24 dims bf16 25.4 / 21.4,
+    // fp32 25.1 / 20.4, of 40 26.3 / 23.0 and 28.7 / 26.4, of 50 29.5 / 26.7 and 36.9 / 38.1; of 72 39 / 72 and 43 / 54, of 100 48 / 83 and
+    // 59 / 73; 512 tokens of 40 dims 8.8 / 7.8 and 8.5 / 7.2, of 50 9.8 / 9.0 and 9.5 / 8.0, of 72 10.4 / 13.0 and 9.4 / 10.8).
+    if (kv.D <= 64) return launch_blocks<kBf16, Turned::Any>(qkv, inv_freq, kv, s, q, stream);
     return launch_blocks<kBf16, Turned::Odd>(qkv, inv_freq, kv, s, q, stream);
 }
 
