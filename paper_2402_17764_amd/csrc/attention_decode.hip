@@ -202,15 +202,17 @@ hipError_t launch_decode(const DecodeArgs& a, const Parts& parts, const KvView& 
 // How many workgroups share a row at most, by the length that the page tables have room for.  A CU draws 25 to 45 bytes a cycle,
 // whatever number of waves asks, and a second launch costs 4 us in a chain of launches: so rows are shared where there are fewer
 // than 256 and more than 1023 tokens (one token, 32 heads of 128, a key-value head each, 1000 tokens: 13.4 us in one launch, 10.0 shared;
-// 64 heads over 8, 500 tokens 7.5 / 9.5, 1000 tokens 9.4 / 9.4), until there are two for each CU (three sequences of 23000 to 41000
-// tokens, 64 heads over 8: 512 workgroups 74.7 us, 1024 79.1, 2048 79.2, none shared 359).  More rows are shared only at every
-// 8192 tokens, so that one long sequence among short ones is not what the call waits for.
+// 64 heads over 8, 500 tokens 7.5 / 9.5, 1000 tokens 9.4 / 9.4), until there are as many as the CUs hold at a time: two each (three
+// sequences of 23000 to 41000 tokens, 64 heads over 8: 512 workgroups 74.7 us, 1024 79.1, 2048 79.2, none shared 359), of heads of more than 128
+// dims, whose registers leave room for one, one each (one sequence of 32000 tokens, 32 heads of 160 over 8, 256 / 512 workgroups 35.0 /
+// 42.4, of 256 dims 47.3 / 53.4; three of 3000, 16 heads of 160 21.9 / 26.8).  More rows are shared only at every 8192 tokens,
+// so that one long sequence among short ones is not what the call waits for.
 struct Splits { int n, least; };
 Splits decode_splits(const KvView& kv, int heads) {
     const int64_t rows = (int64_t)kv.B * kv.kv_heads * ceil_div(heads / kv.kv_heads, 16);
     constexpr int kShort = 8, kLong = 256;                 // blocks: two for each wave of a workgroup; 8192 tokens
     if (kv.max_blocks < 32) return {1, 1};
-    const int64_t fill = rows < 256 ? 512 / rows : 1, long_ones = ceil_div(kv.max_blocks, kLong), room = 8192 / rows;
+    const int64_t fill = rows < 256 ? (kv.D <= 128 ? 512 : 256) / rows : 1, long_ones = ceil_div(kv.max_blocks, kLong), room = 8192 / rows;
     const int least = fill > 1 ? kShort : kLong / 2;
     int64_t n = fill > long_ones ? fill : long_ones < room ? long_ones : room;
     const int64_t most = ceil_div(kv.max_blocks, least);
