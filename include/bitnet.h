@@ -556,7 +556,7 @@ bitnet_status bitnet_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, con
  * divisor takes the weights so too).
  *   q          [rows][heads][head_dim] BF16, 2-byte aligned, as bitnet_rope_kv_append writes it
  *   scale      > 0 and finite (BITNET_ERR_SHAPE otherwise), ordinarily 1/sqrt(head_dim); scores times scale have to be finite fp32 as well
- *   o          out [rows][heads*head_dim], F32 or BF16, element-aligned: what bitnet_quantize_acts or bitnet_linear_fused takes next
+ *   o          out [rows][heads*head_dim], F32 or BF16, element-aligned, not overlapping q: what bitnet_quantize_acts or bitnet_linear_fused takes next
  *   workspace  device memory, 16-byte aligned, or NULL: contents are scratch; calls that share it must not overlap.  With the
  *              bitnet_attention_workspace() bytes or more, few rows on long sequences are spread over the chip: parts of a sequence are
  *              summed up by different workgroups and joined by a second launch

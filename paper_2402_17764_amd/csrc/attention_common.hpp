@@ -115,9 +115,9 @@ __device__ inline void weights_pair(v8bf* w, int j, float p0, float p1) {
 
 // The sum of a row's weights takes them as the values' product does, rounded, so that the rounding of a weight that outweighs the
 // others is in both and goes out of their quotient: values that are all alike come back as they are.  The decode kernel does it as a product with
-// ones, which every lane of a query's four groups gets, in all four places.  The prefill kernel has not the ten registers for that and adds a
-// lane's weights two at a time (the weights as they were before the rounding: results off by another half step; us, those / these: 40 heads
-// of 128, 2048 tokens 58.1 / 57.2, 64 heads over 8, 1024 behind 15000 463 / 445, 32 heads, 4096 tokens 138 / 142, of 64 dims 92 / 95).
+// ones, which every lane of a query's four groups gets, in all four places.  The prefill kernel, whose tiles of 128 rows have not the ten
+// registers for that, adds a lane's weights two at a time (the weights as they were before the rounding: results off by another half step;
+// us, those / these: 40 heads of 128, 2048 tokens 58.1 / 57.2, 64 heads over 8, 1024 behind 15000 463 / 445, 32 heads, 4096 tokens 138 / 142, of 64 dims 92 / 95).
 __device__ inline v8bf ones_operand() {
     v8bf w;
 #pragma unroll
