@@ -550,10 +550,10 @@ bitnet_status bitnet_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, con
 /*
  * o = softmax(scale q . k) v over the cached keys and values of each row's sequence; query head i reads key-value head i / (heads/kv_heads).
  * The row at position pos sees the keys of positions 0 .. pos, whatever memory holds behind them: what is not finite there, or in values of
- * later positions, reaches no row that does not see it.  A row that sees a value that is not finite, or whose sum over values is none in fp32, has
- * NaN in that dim of the heads that read it.  Scores, weights' sums and the sums over values are fp32.  Weights enter their product in bf16: for an F32 result as the sum of three, which hold all 24 bits of a weight; for a
- * BF16 result bitnet_attention_decode takes the sum of two (2^-17 of a weight is left out), bitnet_attention_prefill one (up to 2^-8; the
- * divisor takes the weights so too).
+ * later positions, reaches no row that does not see it.  A row that sees a value that is not finite, or whose sum over values passes fp32, has NaN
+ * in that dim of the heads that read it.  Scores, weights' sums and the sums over values are fp32.  Weights enter their product in bf16: for an
+ * F32 result as the sum of three, which hold all 24 bits of a weight; for a BF16 result bitnet_attention_decode takes the sum of two (2^-17 of a
+ * weight is left out), bitnet_attention_prefill one (up to 2^-8; the divisor takes the weights so too).
  *   q          [rows][heads][head_dim] BF16, 2-byte aligned, as bitnet_rope_kv_append writes it
  *   scale      > 0 and finite (BITNET_ERR_SHAPE otherwise), ordinarily 1/sqrt(head_dim); scores times scale have to be finite fp32 as well
  *   o          out [rows][heads*head_dim], F32 or BF16, element-aligned, not overlapping q: what bitnet_quantize_acts or bitnet_linear_fused takes next
