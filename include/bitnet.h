@@ -569,6 +569,70 @@ bitnet_status bitnet_attention_decode(const void* q, const bitnet_kv* kv, int64_
 bitnet_status bitnet_attention_prefill(const void* q, const bitnet_kv* kv, int64_t T, int64_t heads, float scale, void* o,
                                        bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * bitnet_rope_kv_append with a norm of every query and key head in front, in the same pass: x -> x / sqrt(mean(x^2) + eps) * gain over the head's dims,
+ * then the turn.  Values are not normed.  The mean of the squares is fp64, everything behind it fp32, the result rounded once; a head of zeros stays zeros.
+ *   norm            0: no norm (the gains and eps are ignored)
+ *   q_gain, k_gain  [head_dim] float (device), one for all heads of queries and of keys, or NULL for no gain
+ *   eps             >= 0 and finite (BITNET_ERR_SHAPE otherwise)
+ *   shift           [B] int32 (device) or NULL: a row's angles are those of its position in the cache plus its sequence's shift -- the tokens that
+ *                   bitnet_kv_evict threw out of it
+ *   everything else as bitnet_rope_kv_append takes it.  One launch.
+ */
+bitnet_status bitnet_norm_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, int norm, const float* q_gain, const float* k_gain, float eps,
+                                         const float* inv_freq, int64_t rotary_dims, int pairs, const int32_t* shift, const bitnet_kv* kv, int64_t T,
+                                         int64_t heads, void* q, void* stream);
+
+/*
+ * bitnet_attention_decode for a batch in which runs of sequences have their first tokens in common (a system prompt, a document): these are read once for
+ * all of a run's sequences.
+ *   prefix_start   [prefixes+1] int32 (device), not falling: sequences prefix_start[i] .. prefix_start[i+1]-1 share their first tokens; a sequence in
+ *                  no run shares none
+ *   prefix_len     [prefixes] int32 (device): how many; lengths outside 0 ... max_pages*page_tokens count as the nearest of the two.  They lie on the pages
+ *                  that the table row of the run's first sequence names; the others' rows are read for the tokens behind them alone, so a
+ *                  page that the prefix fills in part may be another one in each row.  A sequence of fewer tokens sees those it has.
+ *   prefixes       at least 1, prefixes*heads < 2^22 (BITNET_ERR_SHAPE otherwise); runs may be empty
+ *   workspace      device memory, 16-byte aligned, of the bitnet_attention_shared_workspace() bytes or more (BITNET_ERR_WORKSPACE otherwise; it is needed here)
+ *   Weights enter their product as in bitnet_attention_prefill for the shared tokens, as in bitnet_attention_decode for a sequence's own.
+ *   kv->q_start is not read.
+ */
+bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, size_t* bytes);
+bitnet_status bitnet_attention_decode_shared(const void* q, const bitnet_kv* kv, const int32_t* prefix_start, const int32_t* prefix_len, int64_t prefixes,
+                                             int64_t heads, float scale, void* o, bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bitnet_attention_decode and bitnet_attention_prefill that also add up what weight each cached token has had:
+ *   weights[b][h][j] += sum over the call's rows of sequence b, and the query heads that read key-value head h, of the softmax weight of token j.
+ *   weights         [B][kv_heads] rows of weights_stride floats (device), weights_stride >= max_pages*page_tokens.  Tokens 0 .. kv_len[b]-1 are updated; the
+ *                   call's own new ones begin with nothing, whatever stood there.  Fp32, from weights that are not rounded; sums in a fixed order.
+ *   workspace       device memory, 16-byte aligned, of the bitnet_attention_weights_workspace() bytes or more (BITNET_ERR_WORKSPACE otherwise; it is needed
+ *                   here): for single tokens 4 bytes for each query head and token that the tables have room for, for runs 8 for each row and head
+ */
+bitnet_status bitnet_attention_weights_workspace(const bitnet_kv* kv, int64_t T, int64_t heads, int prefill, bitnet_dtype o_dtype, size_t* bytes);
+bitnet_status bitnet_attention_decode_weights(const void* q, const bitnet_kv* kv, int64_t heads, float scale, void* o, bitnet_dtype o_dtype, float* weights,
+                                              int64_t weights_stride, void* workspace, size_t workspace_bytes, void* stream);
+bitnet_status bitnet_attention_prefill_weights(const void* q, const bitnet_kv* kv, int64_t T, int64_t heads, float scale, void* o, bitnet_dtype o_dtype,
+                                               float* weights, int64_t weights_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated weight.  Of each sequence and key-value head stay its `recent` last tokens and the keep - recent of the others that have had the
+ * most weight (of equal ones those at the lower positions; what is no number counts as more than all others) -- of a sequence of up to `keep` tokens
+ * all -- in their order.  Their keys, values and weights go to positions 0, 1, ... of the pages that table_out names; the cache's other pages are not touched,
+ * nor the places behind a sequence's new length.  Keys keep the turn of their old positions, and a head's tokens need not be another's:
+ * kv_len_out is what later calls take as kv_len, and old length - new length what they add to `shift` (bitnet_norm_rope_kv_append).
+ *   weights         as above
+ *   keep, recent    1 <= keep < 2^31 - 64, 0 <= recent <= keep
+ *   table_out       [B] rows of int32 page numbers (device), table_out_stride apart, with room for min(keep, max_pages*page_tokens) tokens.  None may be a
+ *                   page that a sequence of the call has its tokens on, none be named twice.  On a page that is not there nothing is stored; a token from
+ *                   a page that is not there is zeros.
+ *   weights_out     [B][kv_heads] rows of weights_out_stride floats, >= min(keep, max_pages*page_tokens); `weights` itself, with its stride, is allowed
+ *   kv_len_out      [B] int32: min(length, keep); kv_len itself is allowed
+ *   kept            [B][kv_heads][keep] int32: the old positions; entries from kv_len_out[b] on are left as they were
+ *   kv->v, kv->k are read and written; kv->q_start is not read.  Two launches.
+ */
+bitnet_status bitnet_kv_evict(const bitnet_kv* kv, const float* weights, int64_t weights_stride, int64_t keep, int64_t recent, const int32_t* table_out,
+                              int64_t table_out_stride, float* weights_out, int64_t weights_out_stride, int32_t* kv_len_out, int32_t* kept, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,8 @@ SYMBOLS = [
     "bitnet_entry_describe", "bitnet_abs_sum", "bitnet_quantize_weights_sharded", "bitnet_quantize_weights_static",
     "bitnet_repack_weights", "bitnet_linear_workspace_format", "bitnet_kv_cache_bytes", "bitnet_rope_kv_append",
     "bitnet_attention_workspace", "bitnet_attention_decode", "bitnet_attention_prefill",
+    "bitnet_norm_rope_kv_append", "bitnet_attention_shared_workspace", "bitnet_attention_decode_shared", "bitnet_attention_weights_workspace",
+    "bitnet_attention_decode_weights", "bitnet_attention_prefill_weights", "bitnet_kv_evict",
 ]
 
 
@@ -105,6 +107,13 @@ def load():
     lib.bitnet_attention_workspace.argtypes = [kvp, i64, i64, ci, szp]
     lib.bitnet_attention_decode.argtypes = [vp, kvp, i64, ctypes.c_float, vp, ci, vp, sz, vp]
     lib.bitnet_attention_prefill.argtypes = [vp, kvp, i64, i64, ctypes.c_float, vp, ci, vp, sz, vp]
+    lib.bitnet_norm_rope_kv_append.argtypes = [vp, ci, ci, vp, vp, ctypes.c_float, vp, i64, ci, vp, kvp, i64, i64, vp, vp]
+    lib.bitnet_attention_shared_workspace.argtypes = [kvp, i64, i64, szp]
+    lib.bitnet_attention_decode_shared.argtypes = [vp, kvp, vp, vp, i64, i64, ctypes.c_float, vp, ci, vp, sz, vp]
+    lib.bitnet_attention_weights_workspace.argtypes = [kvp, i64, i64, ci, ci, szp]
+    lib.bitnet_attention_decode_weights.argtypes = [vp, kvp, i64, ctypes.c_float, vp, ci, vp, i64, vp, sz, vp]
+    lib.bitnet_attention_prefill_weights.argtypes = [vp, kvp, i64, i64, ctypes.c_float, vp, ci, vp, i64, vp, sz, vp]
+    lib.bitnet_kv_evict.argtypes = [kvp, vp, i64, i64, i64, vp, i64, vp, i64, vp, vp, vp]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = ci
     try:
@@ -373,14 +382,43 @@ def rope_kv_append(qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q
     return _native().rope_kv_append(qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_start, pairs, q)
 
 
+def norm_rope_kv_append(qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_gain=None, k_gain=None, eps=1e-6, q_start=None, pairs=False,
+                        norm=True, shift=None, q=None):
+    """rope_kv_append with a norm of every query and key head in front (root of the mean square; gains float32 [D] or None), in the same pass.  shift
+    int32 [B]: how far the rotary positions are ahead of the places in the cache, the tokens that kv_evict threw out."""
+    return _native().norm_rope_kv_append(qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_gain, k_gain, eps, q_start, pairs, norm, shift, q)
+
+
+def _kv_for_query(head_dim, k_cache, page_table, prefill=False):
+    one = 16                                   # stands for the device pointers, which a query does not read
+    return KvStruct(one, one, k_cache.shape[0], 32 * k_cache.shape[2], k_cache.shape[1], head_dim, page_table.shape[0], one, page_table.shape[1],
+                    page_table.shape[1], one, one if prefill else None)
+
+
 def attention_workspace(T, heads, head_dim, k_cache, page_table, prefill=False):
     """Bytes of scratch with which attention_decode (or attention_prefill) may spread few rows on long sequences over the chip (0: none)."""
     lib = load()
-    one = 16                                   # stands for the device pointers, which the query does not read
-    kv = KvStruct(one, one, k_cache.shape[0], 32 * k_cache.shape[2], k_cache.shape[1], head_dim, page_table.shape[0], one, page_table.shape[1],
-                  page_table.shape[1], one, one if prefill else None)
     out = ctypes.c_size_t(0)
-    _check(lib.bitnet_attention_workspace(ctypes.byref(kv), T, heads, int(prefill), ctypes.byref(out)), "bitnet_attention_workspace")
+    _check(lib.bitnet_attention_workspace(ctypes.byref(_kv_for_query(head_dim, k_cache, page_table, prefill)), T, heads, int(prefill), ctypes.byref(out)),
+           "bitnet_attention_workspace")
+    return int(out.value)
+
+
+def attention_shared_workspace(prefixes, heads, head_dim, k_cache, page_table):
+    """Bytes of scratch that attention_decode_shared needs."""
+    lib = load()
+    out = ctypes.c_size_t(0)
+    _check(lib.bitnet_attention_shared_workspace(ctypes.byref(_kv_for_query(head_dim, k_cache, page_table)), prefixes, heads, ctypes.byref(out)),
+           "bitnet_attention_shared_workspace")
+    return int(out.value)
+
+
+def attention_weights_workspace(T, heads, head_dim, k_cache, page_table, prefill=False, y_dtype=BF16):
+    """Bytes of scratch that attention_decode_weights (or attention_prefill_weights) needs."""
+    lib = load()
+    out = ctypes.c_size_t(0)
+    _check(lib.bitnet_attention_weights_workspace(ctypes.byref(_kv_for_query(head_dim, k_cache, page_table, prefill)), T, heads, int(prefill), y_dtype,
+                                                  ctypes.byref(out)), "bitnet_attention_weights_workspace")
     return int(out.value)
 
 
@@ -394,6 +432,30 @@ def attention_prefill(q, k_cache, v_cache, page_table, kv_len, q_start, scale=No
     """Causal attention of runs of new tokens, q [T, heads, D] bfloat16 dealt out by q_start [B + 1], over their sequences' caches, which hold
     the new tokens already -> y [T, heads D]."""
     return _native().attention_prefill(q, k_cache, v_cache, page_table, kv_len, q_start, scale, y_dtype, y, workspace)
+
+
+def attention_decode_shared(q, k_cache, v_cache, page_table, kv_len, prefix_start, prefix_len, scale=None, y_dtype=BF16, y=None, workspace=None):
+    """attention_decode where sequences prefix_start[i] ... prefix_start[i + 1] - 1 share their first prefix_len[i] tokens (int32 [G + 1] and [G]), which
+    are read once for all of them, through the table row of the first."""
+    return _native().attention_decode_shared(q, k_cache, v_cache, page_table, kv_len, prefix_start, prefix_len, scale, y_dtype, y, workspace)
+
+
+def attention_decode_weights(q, k_cache, v_cache, page_table, kv_len, weights, scale=None, y_dtype=BF16, y=None, workspace=None):
+    """attention_decode that adds the softmax weight of each cached token, summed over the heads that read its key-value head, to weights
+    [B, kv heads, tokens] (float32, updated in place; a new token begins with nothing) -> y."""
+    return _native().attention_decode_weights(q, k_cache, v_cache, page_table, kv_len, None, weights, scale, y_dtype, y, workspace)
+
+
+def attention_prefill_weights(q, k_cache, v_cache, page_table, kv_len, q_start, weights, scale=None, y_dtype=BF16, y=None, workspace=None):
+    """attention_prefill that does the same for its runs of new tokens."""
+    return _native().attention_prefill_weights(q, k_cache, v_cache, page_table, kv_len, q_start, weights, scale, y_dtype, y, workspace)
+
+
+def kv_evict(k_cache, v_cache, page_table, kv_len, weights, keep, recent, page_table_out, kv_len_out=None, weights_out=None, kept=None):
+    """Cuts each sequence to `keep` tokens a key-value head: its `recent` last ones and those of the others with the most weight, in their order, on the
+    pages of page_table_out [B, pages], none of which holds tokens of the call's sequences.  -> (kv_len_out int32 [B], weights_out float32 [B, kv heads,
+    tokens], kept int32 [B, kv heads, keep]: the old positions); behind a sequence's new length both are as they were."""
+    return _native().kv_evict(k_cache, v_cache, page_table, kv_len, weights, keep, recent, page_table_out, kv_len_out, weights_out, kept)
 
 
 def unpack_weights(packed, N, K, fmt=PACK_2BIT, codes=None):

@@ -16,7 +16,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbitnet_hip.so")
 
 SOURCES = ["api.hip", "quant_weights.hip", "quant_acts.hip", "linear_ref.hip", "linear_gemv.hip", "linear_decode.hip", "linear_skinny.hip", "linear_ksplit.hip", "linear_gemm.hip", "trit5.hip", "static_scratch.hip",
-           "rope_append.hip", "attention_decode.hip", "attention_prefill.hip", "attention_join.hip"]
+           "rope_append.hip", "attention_decode.hip", "attention_prefill.hip", "attention_join.hip",
+           "norm_rope_append.hip", "attention_shared.hip", "attention_weights.hip", "kv_evict.hip"]
 SOURCES += ["attention_prefill_%d.hip" % d for d in (32, 64, 96, 128, 192, 256)]
 SOURCES += ["attention_prefill_%d_padded.hip" % d for d in (16, 32, 48, 64, 80, 96, 112, 128, 192, 256)]
 SOURCES += ["decode%s_%s.hip" % (k, t) for k in ("", "_norm", "_pair", "_norm_pair") for t in ("bf16", "f32")]

@@ -661,4 +661,100 @@ bitnet_status bitnet_attention_prefill(const void* q, const bitnet_kv* kv, int64
                                                      workspace ? workspace_bytes : 0, static_cast<hipStream_t>(stream)));
 }
 
+bitnet_status bitnet_norm_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype, int norm, const float* q_gain, const float* k_gain, float eps,
+                                         const float* inv_freq, int64_t rotary_dims, int pairs, const int32_t* shift, const bitnet_kv* kv, int64_t T,
+                                         int64_t heads, void* q, void* stream) {
+    if (!qkv || !q || (!inv_freq && rotary_dims != 0)) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    const bitnet_status st = kv_view(kv, T, heads, &view);
+    if (st != BITNET_OK) return st;
+    if (rotary_dims < 0 || rotary_dims > view.D || rotary_dims % 2 || (!view.q_start && T != view.B)) return BITNET_ERR_SHAPE;
+    if (norm && (!(eps >= 0.0f) || !isfinite(eps))) return BITNET_ERR_SHAPE;
+    if (qkv_dtype != BITNET_F32 && qkv_dtype != BITNET_BF16) return BITNET_ERR_DTYPE;
+    if (!aligned(qkv, dtype_size(qkv_dtype)) || !aligned(q, 2) || !aligned(inv_freq, 4) || !aligned(shift, 4)) return BITNET_ERR_ALIGN;
+    if (norm && (!aligned(q_gain, 4) || !aligned(k_gain, 4))) return BITNET_ERR_ALIGN;
+    return from_hip(bitnet::launch_norm_rope_append(qkv, qkv_dtype == BITNET_BF16, norm != 0, q_gain, k_gain, eps, inv_freq, (int)rotary_dims, pairs != 0, shift,
+                                                    view, T, (int)heads, q, static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, size_t* bytes) {
+    if (!bytes) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    const bitnet_status st = kv_view(kv, kv ? kv->sequences : 1, heads, &view);
+    if (st != BITNET_OK) return st;
+    if (prefixes <= 0 || prefixes > kMaxSequenceHeads / heads) return BITNET_ERR_SHAPE;
+    *bytes = bitnet::attention_shared_workspace_bytes(view, (int)prefixes, (int)heads);
+    return BITNET_OK;
+}
+
+bitnet_status bitnet_attention_decode_shared(const void* q, const bitnet_kv* kv, const int32_t* prefix_start, const int32_t* prefix_len, int64_t prefixes,
+                                             int64_t heads, float scale, void* o, bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!prefix_start || !prefix_len || !workspace) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    const bitnet_status st = attention_checked(q, kv, kv ? kv->sequences : 1, heads, scale, o, o_dtype, workspace, &view);
+    if (st != BITNET_OK) return st;
+    if (prefixes <= 0 || prefixes > kMaxSequenceHeads / heads) return BITNET_ERR_SHAPE;
+    if (!aligned(prefix_start, 4) || !aligned(prefix_len, 4)) return BITNET_ERR_ALIGN;
+    if (workspace_bytes < bitnet::attention_shared_workspace_bytes(view, (int)prefixes, (int)heads)) return BITNET_ERR_WORKSPACE;
+    return from_hip(bitnet::launch_attention_shared(q, view, prefix_start, prefix_len, (int)prefixes, (int)heads, scale, o, o_dtype == BITNET_F32, workspace,
+                                                    static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_attention_weights_workspace(const bitnet_kv* kv, int64_t T, int64_t heads, int prefill, bitnet_dtype o_dtype, size_t* bytes) {
+    if (!bytes) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    const bitnet_status st = kv_view(kv, T, heads, &view);
+    if (st != BITNET_OK) return st;
+    if (o_dtype != BITNET_F32 && o_dtype != BITNET_BF16) return BITNET_ERR_DTYPE;
+    *bytes = bitnet::attention_weights_workspace_bytes(view, T, (int)heads, prefill != 0, o_dtype == BITNET_F32);
+    return BITNET_OK;
+}
+
+static bitnet_status weights_checked(const bitnet::KvView& kv, const float* weights, int64_t stride) {
+    if (stride < (int64_t)kv.max_blocks * bitnet::kKvBlock || stride > kMaxElems / kv.kv_heads / kv.B) return BITNET_ERR_SHAPE;
+    return aligned(weights, 4) ? BITNET_OK : BITNET_ERR_ALIGN;
+}
+
+bitnet_status bitnet_attention_decode_weights(const void* q, const bitnet_kv* kv, int64_t heads, float scale, void* o, bitnet_dtype o_dtype, float* weights,
+                                              int64_t weights_stride, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!weights || !workspace) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    bitnet_status st = attention_checked(q, kv, kv ? kv->sequences : 1, heads, scale, o, o_dtype, workspace, &view);
+    if (st == BITNET_OK) st = weights_checked(view, weights, weights_stride);
+    if (st != BITNET_OK) return st;
+    if (workspace_bytes < bitnet::attention_weights_workspace_bytes(view, view.B, (int)heads, false, o_dtype == BITNET_F32)) return BITNET_ERR_WORKSPACE;
+    return from_hip(bitnet::launch_attention_decode_weights(q, view, (int)heads, scale, o, o_dtype == BITNET_F32, weights, weights_stride, workspace,
+                                                            static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_attention_prefill_weights(const void* q, const bitnet_kv* kv, int64_t T, int64_t heads, float scale, void* o, bitnet_dtype o_dtype,
+                                               float* weights, int64_t weights_stride, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!weights || !workspace) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    bitnet_status st = attention_checked(q, kv, T, heads, scale, o, o_dtype, workspace, &view);
+    if (st == BITNET_OK) st = weights_checked(view, weights, weights_stride);
+    if (st != BITNET_OK) return st;
+    if (!view.q_start) return BITNET_ERR_NULL;
+    if (workspace_bytes < bitnet::attention_weights_workspace_bytes(view, T, (int)heads, true, o_dtype == BITNET_F32)) return BITNET_ERR_WORKSPACE;
+    return from_hip(bitnet::launch_attention_prefill_weights(q, view, T, (int)heads, scale, o, o_dtype == BITNET_F32, weights, weights_stride, workspace,
+                                                             workspace_bytes, static_cast<hipStream_t>(stream)));
+}
+
+bitnet_status bitnet_kv_evict(const bitnet_kv* kv, const float* weights, int64_t weights_stride, int64_t keep, int64_t recent, const int32_t* table_out,
+                              int64_t table_out_stride, float* weights_out, int64_t weights_out_stride, int32_t* kv_len_out, int32_t* kept, void* stream) {
+    if (!weights || !table_out || !weights_out || !kv_len_out || !kept) return BITNET_ERR_NULL;
+    bitnet::KvView view;
+    bitnet_status st = kv_view(kv, kv ? kv->sequences : 1, kv ? kv->kv_heads : 1, &view);
+    if (st == BITNET_OK) st = weights_checked(view, weights, weights_stride);
+    if (st != BITNET_OK) return st;
+    const int64_t room = (int64_t)view.max_blocks * bitnet::kKvBlock, most = keep < room ? keep : room;
+    if (keep <= 0 || keep >= ((int64_t)1 << 31) - 64 || recent < 0 || recent > keep) return BITNET_ERR_SHAPE;
+    if (table_out_stride < bitnet::ceil_div(most, kv->page_tokens) || table_out_stride > kMaxElems / view.B) return BITNET_ERR_SHAPE;
+    if (weights_out_stride < most || weights_out_stride > kMaxElems / view.kv_heads / view.B || keep > kMaxElems / view.kv_heads / view.B) return BITNET_ERR_SHAPE;
+    if (weights_out == weights && weights_out_stride != weights_stride) return BITNET_ERR_SHAPE;
+    if (!aligned(table_out, 4) || !aligned(weights_out, 4) || !aligned(kv_len_out, 4) || !aligned(kept, 4)) return BITNET_ERR_ALIGN;
+    return from_hip(bitnet::launch_kv_evict(view, weights, weights_stride, (int)keep, (int)recent, table_out, table_out_stride, weights_out, weights_out_stride,
+                                            kv_len_out, kept, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

@@ -4,6 +4,8 @@
 #include "bitnet_internal.hpp"
 #include "kv_layout.hpp"
 
+#include <type_traits>
+
 namespace bitnet {
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -142,6 +144,12 @@ __device__ inline void values_keep(v4u& v, int count) {
     for (int w = 0; w < 4; ++w) v[w] &= count >= 2 * w + 2 ? 0xFFFFFFFFu : count == 2 * w + 1 ? 0x0000FFFFu : 0u;
 }
 
+// ... and which of them do not: the first `count`, which are read elsewhere
+__device__ inline void values_drop(v4u& v, int count) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[w] &= count >= 2 * w + 2 ? 0u : count == 2 * w + 1 ? 0xFFFF0000u : 0xFFFFFFFFu;
+}
+
 // A sum over values times `by`: NaN where the sum is an infinity.  An infinite value that a row sees meets weights of zero and factors of zero (0 inf) in some
 // tiles, splits and types and in others not, and what is noted of it where a tile ends (prefill) is NaN: so all of them say NaN.
 __device__ inline float finite_or_nan(float sum, float by) { return __builtin_fmaf(sum, 0.0f, sum * by); }
@@ -189,7 +197,12 @@ struct JoinArgs {
     float scale;                       // of the softmax, times log2 e
     int heads, group, T, rows_a_tile;
 };
-hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream);
+// Where rows leave their softmax states, m and l of weights that are not rounded.
+struct KeptRows {
+    float* state = nullptr;            // [rows][2]
+    float* totals = nullptr;           // of the splits, as Parts' places: l of weights that are not rounded; NULL where Parts' l is that already
+};
+hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream, const KeptRows& keep = KeptRows());
 
 // The prefill kernel's tile of a sequence's rows for one head: the keys that its last token sees, and how many 64 tokens of them (the unit in
 // which they are shared out).
@@ -199,5 +212,22 @@ __device__ inline int tile_sees(const NewTokens& nt, int row_last, int group) { 
 __device__ inline int stages_of(int seen) { return seen > 0 ? (seen + kStageTokens - 1) / kStageTokens : 0; }
 
 __device__ inline int blocks_of(const KvView& kv, int b) { return (kv.length(kv.kv_len[b]) + kKvBlock - 1) / kKvBlock; }
+
+// The kernel for a head's size: `go` is called with the sizes that it is built for, kC chunks of 32 dims and kV tiles of 16, as types
+template <typename Go>
+hipError_t for_head_size(int D, Go go) {
+    const int chunks = (D + 31) / 32;
+    const bool exact = D % 32 == 0, one_tile = D % 32 != 0 && D % 32 <= 16;
+#define SIZE(kC_, kV_, kE_) return go(std::integral_constant<int, kC_>(), std::integral_constant<int, kV_>(), std::integral_constant<bool, kE_>())
+    switch (chunks) {
+        case 1: if (exact) SIZE(1, 2, true); if (one_tile) SIZE(1, 1, false); SIZE(1, 2, false);
+        case 2: if (exact) SIZE(2, 4, true); if (one_tile) SIZE(2, 3, false); SIZE(2, 4, false);
+        case 3: if (exact) SIZE(3, 6, true); if (one_tile) SIZE(3, 5, false); SIZE(3, 6, false);
+        case 4: if (exact) SIZE(4, 8, true); if (one_tile) SIZE(4, 7, false); SIZE(4, 8, false);
+        case 5: case 6: if (exact && chunks == 6) SIZE(6, 12, true); SIZE(6, 12, false);
+        default: if (exact && chunks == 8) SIZE(8, 16, true); SIZE(8, 16, false);
+    }
+#undef SIZE
+}
 
 }  // namespace bitnet

@@ -1,23 +1,10 @@
 // The second launch of attention whose rows were shared by several workgroups: one query head of one row to a workgroup.
-#include "attention_common.hpp"
+#include "attention_join.hpp"
+
+#include <type_traits>
 
 namespace bitnet {
 namespace {
-
-__device__ inline float wave_max(float v) {
-    v = fmaxf(v, dpp_f32<0xB1>(v));
-    v = fmaxf(v, dpp_f32<0x4E>(v));
-    v = fmaxf(v, dpp_f32<0x141>(v));
-    v = fmaxf(v, dpp_f32<0x140>(v));
-    return groups_max(v);
-}
-__device__ inline float wave_sum(float v) {
-    v += dpp_f32<0xB1>(v);
-    v += dpp_f32<0x4E>(v);
-    v += dpp_f32<0x141>(v);
-    v += dpp_f32<0x140>(v);
-    return groups_sum(v);
-}
 
 // how many splits of a row have been written: as the workgroups that wrote them found it
 __device__ inline int splits_of(const JoinArgs& a, const Parts& parts, const KvView& kv, int t, int head) {
@@ -36,54 +23,31 @@ __device__ inline int splits_of(const JoinArgs& a, const Parts& parts, const KvV
     return (units + run - 1) / run;
 }
 
-template <bool kF32>
-__global__ __launch_bounds__(256) void attention_join(JoinArgs a, Parts parts, KvView kv) {
-    __shared__ float weights[kMostSplits], totals[4], tops[4];
-    __shared__ v4f sums[4][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), D = kv.D, dim = 4 * lane;
+template <bool kF32, bool kKeep>
+__global__ __launch_bounds__(256) void attention_join(JoinArgs a, Parts parts, KvView kv, std::conditional_t<kKeep, KeptRows, char> keep) {
+    __shared__ JoinRoom room;
     const int t = blockIdx.x / a.heads, head = blockIdx.x - t * a.heads;
-    const int64_t place0 = (int64_t)blockIdx.x * parts.splits;
-    auto sums_of = [&](int s) {
-        v4f y = {0, 0, 0, 0};
-        const float* p = parts.sums + (place0 + s) * D + dim;
-        if (dim + 4 <= D) __builtin_memcpy(&y, p, 16);
-        else if (dim < D) { y[0] = p[0]; y[1] = p[1]; }     // heads have an even number of dims
-        return y;
-    };
     const int n = splits_of(a, parts, kv, t, head);
     if (n < 2) return;                                      // stored by the workgroup that had all of it
-    float m = kMinusInf, l = 0.0f;                          // one split a thread: its weight, exp(m_s - m), and its share of l
-    if ((int)threadIdx.x < n) {
-        m = parts.state[(place0 + threadIdx.x) * 2];
-        l = parts.state[(place0 + threadIdx.x) * 2 + 1];
+    if constexpr (kKeep) {
+        const JoinState all = join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, n, 0, a.scale, kv.D, a.o, blockIdx.x, keep.totals);
+        if (threadIdx.x == 0) {
+            keep.state[2 * (int64_t)blockIdx.x] = all.top;
+            keep.state[2 * (int64_t)blockIdx.x + 1] = all.other;
+        }
+    } else {
+        join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, n, 0, a.scale, kv.D, a.o, blockIdx.x);
     }
-    float top = wave_max(m);
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float w = m == kMinusInf ? 0.0f : exp2_fast((m - top) * a.scale);      // of a split that saw no token: 0
-    weights[threadIdx.x] = w;
-    l = wave_sum(l * w);
-    if (lane == 0) totals[wave] = l;
-    __syncthreads();
-    v4f x = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int s = wave; s < n; s += 4) x += sums_of(s) * weights[s];
-    sums[wave][lane] = x;
-    __syncthreads();
-    if (wave != 0 || dim >= D) return;
-    x = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-    const float total = (totals[0] + totals[1]) + (totals[2] + totals[3]), inv = total > 0.0f ? 1.0f / total : 0.0f;
-    const float y[4] = {finite_or_nan(x[0], inv), finite_or_nan(x[1], inv), finite_or_nan(x[2], inv), finite_or_nan(x[3], inv)};
-    store4<kF32>(a.o, (int64_t)blockIdx.x * D, dim, D, y);
 }
 
 }  // namespace
 
-hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream) {
+hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream, const KeptRows& keep) {
     const unsigned rows = (unsigned)((int64_t)a.T * a.heads);
-    if (f32) attention_join<true><<<rows, 256, 0, stream>>>(a, parts, kv);
-    else attention_join<false><<<rows, 256, 0, stream>>>(a, parts, kv);
+    if (f32 && keep.state) attention_join<true, true><<<rows, 256, 0, stream>>>(a, parts, kv, keep);
+    else if (f32) attention_join<true, false><<<rows, 256, 0, stream>>>(a, parts, kv, 0);
+    else if (keep.state) attention_join<false, true><<<rows, 256, 0, stream>>>(a, parts, kv, keep);
+    else attention_join<false, false><<<rows, 256, 0, stream>>>(a, parts, kv, 0);
     return hipGetLastError();
 }
 

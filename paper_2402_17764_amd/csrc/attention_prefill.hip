@@ -3,10 +3,10 @@
 
 namespace bitnet {
 
-#define EXTERN(kC_, kV_, kE_) extern template hipError_t launch_prefill<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t)
-EXTERN(1, 2, true); EXTERN(2, 4, true); EXTERN(3, 6, true); EXTERN(4, 8, true); EXTERN(6, 12, true); EXTERN(8, 16, true);
-EXTERN(1, 1, false); EXTERN(2, 3, false); EXTERN(3, 5, false); EXTERN(4, 7, false);
-EXTERN(1, 2, false); EXTERN(2, 4, false); EXTERN(3, 6, false); EXTERN(4, 8, false); EXTERN(6, 12, false); EXTERN(8, 16, false);
+#define EXTERN(kC_, kV_, kE_)                                                                                                                              \
+    extern template hipError_t launch_prefill<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);                \
+    extern template hipError_t launch_prefill_kept<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, const RowsMore&, hipStream_t);
+BITNET_PREFILL_SIZES(EXTERN)
 #undef EXTERN
 
 struct PrefillPlan { PrefillTile tile; int splits, least; };
@@ -35,30 +35,38 @@ size_t attention_prefill_workspace_bytes(const KvView& kv, int64_t T, int heads)
     return Parts::bytes(T * heads, prefill_plan(kv, T, heads).splits, kv.D);
 }
 
-hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, void* workspace,
-                                    size_t workspace_bytes, hipStream_t stream) {
+// `keep`: rows leave their softmax states there (its totals are set here), if it names a place
+static hipError_t launch_runs(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, KeptRows keep, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
     const float by = scale * 1.44269504f;
     const PrefillArgs a{static_cast<const uint16_t*>(q), o, by, fminf(kSlack / by, 3e38f), heads, heads / kv.kv_heads, (int)T, 0};
     const PrefillPlan plan = prefill_plan(kv, T, heads);
+    const size_t bytes = Parts::bytes(T * heads, plan.splits, kv.D);
     Parts parts;
-    if (plan.splits > 1 && workspace_bytes >= Parts::bytes(T * heads, plan.splits, kv.D)) parts = Parts(workspace, T * heads, plan.splits, plan.least, kv.D);
-    const int chunks = (int)ceil_div(kv.D, 32);
-    const bool exact = kv.D % 32 == 0, one_tile = !exact && kv.D % 32 <= 16;
-    hipError_t e = hipErrorInvalidValue;
-#define PREFILL(kC_, kV_, kE_) e = launch_prefill<kC_, kV_, kE_>(plan.tile, a, parts, kv, f32, stream)
-#define SIZES(kC_) if (exact) PREFILL(kC_, 2 * kC_, true); else if (one_tile) PREFILL(kC_, 2 * kC_ - 1, false); else PREFILL(kC_, 2 * kC_, false); break
-    switch (chunks) {
-        case 1: SIZES(1);
-        case 2: SIZES(2);
-        case 3: SIZES(3);
-        case 4: SIZES(4);
-        case 5: case 6: if (exact && chunks == 6) PREFILL(6, 12, true); else PREFILL(6, 12, false); break;
-        default: if (exact && chunks == 8) PREFILL(8, 16, true); else PREFILL(8, 16, false); break;
+    if (plan.splits > 1 && workspace_bytes >= (keep.state ? attention_prefill_kept_bytes(kv, T, heads, f32) : bytes)) {
+        parts = Parts(workspace, T * heads, plan.splits, plan.least, kv.D);
+        if (keep.state && !f32) keep.totals = reinterpret_cast<float*>(static_cast<char*>(workspace) + bytes);
     }
-#undef SIZES
-#undef PREFILL
+    const hipError_t e = for_head_size(kv.D, [&](auto c, auto v, auto exact) {
+        if (keep.state) return launch_prefill_kept<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, RowsMore{keep, {}, 0}, stream);
+        return launch_prefill<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, stream);
+    });
     if (e != hipSuccess || parts.splits < 2) return e;
-    return launch_attention_join({o, a.scale, heads, a.group, (int)T, prefill_rows(plan.tile)}, parts, kv, f32, stream);
+    return launch_attention_join({o, a.scale, heads, a.group, (int)T, prefill_rows(plan.tile)}, parts, kv, f32, stream, keep);
+}
+
+hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream) {
+    return launch_runs(q, kv, T, heads, scale, o, f32, {}, workspace, workspace_bytes, stream);
+}
+
+size_t attention_prefill_kept_bytes(const KvView& kv, int64_t T, int heads, bool f32) {
+    const int splits = prefill_plan(kv, T, heads).splits;
+    return Parts::bytes(T * heads, splits, kv.D) + (splits < 2 || f32 ? 0 : ((size_t)(T * heads * splits) * 4 + 15) / 16 * 16);
+}
+hipError_t launch_attention_prefill_kept(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, const KeptRows& keep,
+                                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    return launch_runs(q, kv, T, heads, scale, o, f32, keep, workspace, workspace_bytes, stream);
 }
 
 }  // namespace bitnet

@@ -2,5 +2,5 @@
 #include "attention_prefill_kernel.hpp"
 
 namespace bitnet {
-template hipError_t launch_prefill<1, 2, false>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);
+BITNET_PREFILL_UNIT(1, 2, false)
 }

@@ -24,6 +24,16 @@ struct PrefillArgs {
     int tiles;                         // of the launch, per key-value head
 };
 
+// Whose rows a launch takes: runs of new tokens, causal; the same, leaving each row's softmax state (of weights as they are, not as they are rounded)
+// for the weights of the keys; or the single new tokens of sequences that share their first tokens, over those alone, as the first
+// parts of rows that have `pitch` of them.
+enum class Rows { Causal, Kept, Shared };
+struct RowsMore {
+    KeptRows keep;                     // Kept
+    Prefixes prefixes;                 // Shared
+    int pitch;
+};
+
 // The shapes of a workgroup: four waves of one or two times 16 rows each (heads of more than 128 dims: four or eight waves of 16, as a wave's
 // sums take its registers), and stages of LDS of one cache block, or two where a block is small.  Both leave room for three or
 // four workgroups on a CU, which is what hides a stage's barrier and the chain of loads that a workgroup begins with (us, one prompt of
@@ -40,8 +50,8 @@ constexpr float kSlack = 8.0f;         // in the exponent of 2
 // there, and results of such dims are not stored.
 constexpr int prefill_lds(int kC, int kV, int blocks) { return 2 * blocks * (2 * kC + kV) * 1024; }
 
-template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
-__global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(PrefillArgs a, Parts parts, KvView kv) {
+template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32, Rows kOf>
+__global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(PrefillArgs a, Parts parts, KvView kv, std::conditional_t<kOf == Rows::Causal, char, RowsMore> more) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kRows = 16 * kNT * kW, kU = kStageBlocks;   // cache blocks of a stage
     constexpr int kPerUnit = kStageTokens / (kKvBlock * kStageBlocks);
@@ -65,15 +75,24 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     // Heads side by side: with a multiple of eight of them a head's tiles meet on one XCD, whose L2 then holds its keys and values once.
     const int h = blockIdx.x % kv.kv_heads;
     const int64_t x = a.tiles - 1 - (int)(blockIdx.x / kv.kv_heads);       // late tiles, which see most, first
-    const int b = sequence_of_tile(kv.q_start, kv.B, x, a.group, kRows, 1);
-    const NewTokens nt(kv, b, a.T);
+    // of shared rows: a group in a sequence's place, its sequences in that of new tokens
+    const int32_t* start;
+    int b;
+    if constexpr (kOf == Rows::Shared) start = more.prefixes.start, b = sequence_of_tile(start, more.prefixes.groups, x, a.group, kRows, 1);
+    else start = kv.q_start, b = sequence_of_tile(start, kv.B, x, a.group, kRows, 1);
+    const auto nt = [&] {
+        if constexpr (kOf == Rows::Shared) return SharedRows(kv, more.prefixes, b);
+        else return NewTokens(kv, b, a.T);
+    }();
     // tokens times heads are below 2^28, so rows have 32 bits: 64-bit quotients are a hundred instructions each in front of the first load
-    const int64_t tile = x - first_tile(kv.q_start[b], b, a.group, kRows, 1);
+    const int64_t tile = x - first_tile(start[b], b, a.group, kRows, 1);
     const int rows = nt.n * a.group;                                       // of the sequence, for this head
     if (tile < 0 || tile * kRows >= rows) return;
     const int row0 = (int)tile * kRows;
     const int row_last = min(row0 + kRows, rows) - 1;
-    const int seen = tile_sees(nt, row_last, a.group);                     // keys that the tile's last token sees
+    int seen;                                                              // keys that the tile's last token sees, or that all share
+    if constexpr (kOf == Rows::Shared) seen = nt.len;
+    else seen = tile_sees(nt, row_last, a.group);
     const int blocks = seen > 0 ? (seen + kKvBlock - 1) / kKvBlock : 0, all_stages = stages_of(seen);
     // this workgroup's stages
     const int run = parts.run(all_stages), stage0 = blockIdx.y * run * kPerUnit;
@@ -88,13 +107,33 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     for (int n = 0; n < kNT; ++n) {
         const int R = wave_row + 16 * n + r, tok = token_of(R, a.group), hh = R - tok * a.group;
         out_row[n] = R < rows ? (nt.first + tok) * a.heads + h * a.group + hh : -1;
-        pos[n] = R < rows ? nt.pos0 + tok : -1;
+        if constexpr (kOf == Rows::Shared) pos[n] = R < rows ? min(kv.length(kv.kv_len[nt.first + tok]), nt.len) - 1 : -1;
+        else pos[n] = R < rows ? nt.pos0 + tok : -1;
         load_query<kC, kExact>(qf[n], R < rows ? a.q + (int64_t)out_row[n] * D : nullptr, g, D);
     }
-    const int tile_pos = nt.pos0 + token_of(row0, a.group);                 // of the tile's first token, and of the wave's last
-    const int pos_last = wave_row < rows ? nt.pos0 + token_of(min(wave_row + 16 * kNT, rows) - 1, a.group) : -1;
-
-    const int32_t* table = kv.table + b * kv.table_stride;
+    int tile_pos, pos_last;                                                 // of the tile's first token, and of the wave's last
+    const int32_t* table = kv.table;
+    if constexpr (kOf == Rows::Shared) {                                    // the least of the tile, and the most
+        const int tok0 = token_of(row0, a.group), toks = token_of(row_last, a.group) - tok0 + 1;
+        int least = 0x7FFFFFFF, most = 0;
+        for (int i = lane; i < toks; i += 64) {
+            const int n = min(kv.length(kv.kv_len[nt.first + tok0 + i]), nt.len);
+            least = min(least, n);
+            most = max(most, n);
+        }
+#pragma unroll
+        for (int by = 1; by < 64; by *= 2) {
+            least = min(least, __shfl_xor(least, by));
+            most = max(most, __shfl_xor(most, by));
+        }
+        tile_pos = __builtin_amdgcn_readfirstlane(least) - 1;
+        pos_last = wave_row < rows ? __builtin_amdgcn_readfirstlane(most) - 1 : -1;
+        table += nt.first * kv.table_stride;
+    } else {
+        tile_pos = nt.pos0 + token_of(row0, a.group);
+        pos_last = wave_row < rows ? nt.pos0 + token_of(min(wave_row + 16 * kNT, rows) - 1, a.group) : -1;
+        table += b * kv.table_stride;
+    }
     int numbers = -1;                                                      // of 64 blocks, one a lane
     auto fetch_numbers = [&](int blk0) {
         const int blk = blk0 + lane;
@@ -120,6 +159,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 
     v4f acc[kNT][kV];
     float m[kNT], base[kNT], l[kNT];                                       // base: m times scale, or 0; l: of this lane's tokens
+    constexpr bool kBoth = kOf == Rows::Kept && !kF32;                     // another sum, of weights that are not rounded
+    [[maybe_unused]] float whole_l[kNT] = {};
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         m[n] = kMinusInf;
@@ -152,6 +193,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 const float p1 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][(j & 3) + 1], a.scale, -base[n]));
                 weights_pair<kParts>(w[u][n], j, p0, p1);
                 l[n] = kF32 ? l[n] + p0 + p1 : add_rounded(l[n], w[u][n][0], j);
+                if constexpr (kBoth) whole_l[n] += p0 + p1;
             }
         };
         auto scores = [&](int u, int with) {
@@ -214,6 +256,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                     m[n] = now;
                     base[n] = now == kMinusInf ? 0.0f : now * a.scale;
                     l[n] *= by;
+                    if constexpr (kBoth) whole_l[n] *= by;
 #pragma unroll
                     for (int i = 0; i < kV; ++i) acc[n][i] *= by;
                     if (u > 0)
@@ -302,9 +345,12 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         const float total = groups_sum(l[n]), inv = total > 0.0f ? 1.0f / total : 0.0f;
+        [[maybe_unused]] float kept = total;
+        if constexpr (kBoth) kept = groups_sum(whole_l[n]);
         if (out_row[n] < 0) continue;
-        const int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
-        const bool whole = run >= all_stages;
+        int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
+        if constexpr (kOf == Rows::Shared) place = (int64_t)out_row[n] * more.pitch + blockIdx.y;
+        const bool whole = kOf != Rows::Shared && run >= all_stages;
         const float by = whole ? inv : 1.0f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
@@ -319,34 +365,66 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         if (!whole && g == 0) {
             parts.state[2 * place] = m[n];
             parts.state[2 * place + 1] = total;
+            if constexpr (kBoth) more.keep.totals[place] = kept;
         }
+        if constexpr (kOf == Rows::Kept)
+            if (whole && g == 0) {
+                more.keep.state[2 * (int64_t)out_row[n]] = m[n];
+                more.keep.state[2 * (int64_t)out_row[n] + 1] = kept;
+            }
     }
 #endif
 }
 
-template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32>
-hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView& kv, hipStream_t stream) {
+template <int kC, int kV, bool kExact, int kNT, int kStageBlocks, int kW, int kOcc, bool kF32, Rows kOf, typename More>
+hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView& kv, More more, hipStream_t stream) {
     static RaisedFlags raised;
-    const auto kernel = attention_prefill_tiles<kC, kV, kExact, kNT, kStageBlocks, kW, kOcc, kF32>;
+    const auto kernel = attention_prefill_tiles<kC, kV, kExact, kNT, kStageBlocks, kW, kOcc, kF32, kOf>;
     constexpr int kLds = prefill_lds(kC, kV, kStageBlocks);
     if (kLds > 65536 - 2048) {                             // with the static part
         const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds, raised);
         if (e != hipSuccess) return e;
     }
-    a.tiles = (int)tiles_at_most(a.T, kv.B, a.group, 16 * kNT * kW, 1);
-    kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, kLds, stream>>>(a, parts, kv);
+    if constexpr (kOf == Rows::Shared) a.tiles = (int)tiles_at_most(kv.B, more.prefixes.groups, a.group, 16 * kNT * kW, 1);
+    else a.tiles = (int)tiles_at_most(a.T, kv.B, a.group, 16 * kNT * kW, 1);
+    kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, kLds, stream>>>(a, parts, kv, more);
     return hipGetLastError();
 }
-template <int kC, int kV, bool kExact, bool kF32>
-hipError_t launch_prefill_form(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, hipStream_t stream) {
+template <int kC, int kV, bool kExact, bool kF32, Rows kOf, typename More>
+hipError_t launch_prefill_form(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, More more, hipStream_t stream) {
     constexpr int kStageBlocks = kC <= 2 ? 2 : 1;
-    if (tile == PrefillTile::Rows64) return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kC <= 4 ? 4 : 2, kF32>(a, parts, kv, stream);
-    return launch_prefill_tiles<kC, kV, kExact, kC <= 4 ? 2 : 1, kStageBlocks, kC <= 4 ? 4 : 8, kC <= 4 && !kF32 ? 3 : 2, kF32>(a, parts, kv, stream);
+    if (tile == PrefillTile::Rows64) return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kC <= 4 ? 4 : 2, kF32, kOf>(a, parts, kv, more, stream);
+    return launch_prefill_tiles<kC, kV, kExact, kC <= 4 ? 2 : 1, kStageBlocks, kC <= 4 ? 4 : 8, kC <= 4 && !kF32 ? 3 : 2, kF32, kOf>(a, parts, kv, more, stream);
 }
 // compiled in translation units of their own
 template <int kC, int kV, bool kExact>
 hipError_t launch_prefill(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream) {
-    return f32 ? launch_prefill_form<kC, kV, kExact, true>(tile, a, parts, kv, stream) : launch_prefill_form<kC, kV, kExact, false>(tile, a, parts, kv, stream);
+    return f32 ? launch_prefill_form<kC, kV, kExact, true, Rows::Causal>(tile, a, parts, kv, (char)0, stream)
+               : launch_prefill_form<kC, kV, kExact, false, Rows::Causal>(tile, a, parts, kv, (char)0, stream);
 }
+template <int kC, int kV, bool kExact>
+hipError_t launch_prefill_kept(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, bool f32, const RowsMore& more, hipStream_t stream) {
+    return f32 ? launch_prefill_form<kC, kV, kExact, true, Rows::Kept>(tile, a, parts, kv, more, stream)
+               : launch_prefill_form<kC, kV, kExact, false, Rows::Kept>(tile, a, parts, kv, more, stream);
+}
+template <int kC, int kV, bool kExact>
+hipError_t launch_prefill_shared(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, bool f32, const RowsMore& more, hipStream_t stream) {
+    return f32 ? launch_prefill_form<kC, kV, kExact, true, Rows::Shared>(tile, a, parts, kv, more, stream)
+               : launch_prefill_form<kC, kV, kExact, false, Rows::Shared>(tile, a, parts, kv, more, stream);
+}
+
+// The sizes that those units build, and the one for a head of D dims: `go` is called with it as types.
+#define BITNET_PREFILL_SIZES(X) \
+    X(1, 2, true) X(2, 4, true) X(3, 6, true) X(4, 8, true) X(6, 12, true) X(8, 16, true) X(1, 1, false) X(2, 3, false) X(3, 5, false) X(4, 7, false) \
+    X(1, 2, false) X(2, 4, false) X(3, 6, false) X(4, 8, false) X(6, 12, false) X(8, 16, false)
+#define BITNET_PREFILL_UNIT(kC_, kV_, kE_)                                                                                                          \
+    template hipError_t launch_prefill<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, hipStream_t);                \
+    template hipError_t launch_prefill_kept<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, const RowsMore&, hipStream_t); \
+    template hipError_t launch_prefill_shared<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, const RowsMore&, hipStream_t);
+
+// Runs of rows whose softmax states are kept.  keep.totals is taken from the workspace: attention_prefill_kept_bytes.
+size_t attention_prefill_kept_bytes(const KvView& kv, int64_t T, int heads, bool f32);
+hipError_t launch_attention_prefill_kept(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, const KeptRows& keep, void* workspace,
+                                         size_t workspace_bytes, hipStream_t stream);
 
 }  // namespace bitnet

@@ -185,5 +185,20 @@ hipError_t launch_attention_decode(const void* q, const KvView& kv, int heads, f
 size_t attention_prefill_workspace_bytes(const KvView& kv, int64_t T, int heads);
 hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, void* workspace,
                                     size_t workspace_bytes, hipStream_t stream);
+// norm_rope_append.hip: norms of queries and keys in front of that
+hipError_t launch_norm_rope_append(const void* qkv, bool bf16, bool norm, const float* q_gain, const float* k_gain, float eps, const float* inv_freq, int rotary,
+                                   bool pairs, const int32_t* shift, const KvView& kv, int64_t T, int heads, void* q, hipStream_t stream);
+// attention_shared.hip, attention_weights.hip; their workspaces have the queries' bytes
+size_t attention_shared_workspace_bytes(const KvView& kv, int groups, int heads);
+hipError_t launch_attention_shared(const void* q, const KvView& kv, const int32_t* prefix_start, const int32_t* prefix_len, int groups, int heads, float scale,
+                                   void* o, bool f32, void* workspace, hipStream_t stream);
+size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill, bool f32);
+hipError_t launch_attention_decode_weights(const void* q, const KvView& kv, int heads, float scale, void* o, bool f32, float* weights, int64_t stride,
+                                           void* workspace, hipStream_t stream);
+hipError_t launch_attention_prefill_weights(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, float* weights, int64_t stride,
+                                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+// kv_evict.hip
+hipError_t launch_kv_evict(const KvView& kv, const float* weights, int64_t stride, int keep, int recent, const int32_t* table_out, int64_t table_out_stride,
+                           float* weights_out, int64_t stride_out, int32_t* len_out, int32_t* kept, hipStream_t stream);
 
 }  // namespace bitnet

@@ -8,6 +8,7 @@
 // around the call, as ctypes does.
 #include <Python.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include <ATen/ATen.h>
@@ -38,6 +39,13 @@ struct Abi {
     decltype(&bitnet_attention_workspace) attention_workspace;
     decltype(&bitnet_attention_decode) attention_decode;
     decltype(&bitnet_attention_prefill) attention_prefill;
+    decltype(&bitnet_norm_rope_kv_append) norm_rope_kv_append;
+    decltype(&bitnet_attention_shared_workspace) attention_shared_workspace;
+    decltype(&bitnet_attention_decode_shared) attention_decode_shared;
+    decltype(&bitnet_attention_weights_workspace) attention_weights_workspace;
+    decltype(&bitnet_attention_decode_weights) attention_decode_weights;
+    decltype(&bitnet_attention_prefill_weights) attention_prefill_weights;
+    decltype(&bitnet_kv_evict) kv_evict;
 } abi;
 PyObject* error_class = nullptr;
 
@@ -426,32 +434,78 @@ struct Cache {
         return t;
     }
     void* stream() const { return c10::hip::getCurrentHIPStream(x.device().index()).stream(); }
+    // `n` numbers of one dimension, or NULL for None where that is allowed
+    template <typename T>
+    const T* list(PyObject* o, const char* name, at::ScalarType dt, int64_t n, bool none) const {
+        if (none && o == Py_None) return nullptr;
+        const at::Tensor& t = here(o, name, dt);
+        if (t.dim() != 1 || t.size(0) != n) raise(PyExc_ValueError, "%s must have %lld entries", name, (long long)n);
+        return static_cast<const T*>(t.const_data_ptr());
+    }
+    // [sequences, kv heads, tokens]
+    const at::Tensor& weights(PyObject* o, const char* name) const {
+        const at::Tensor& t = here(o, name, at::kFloat);
+        if (t.dim() != 3 || t.size(0) != kv.sequences || t.size(1) != kv.kv_heads)
+            raise(PyExc_ValueError, "%s must be [%lld, %lld, tokens]", name, (long long)kv.sequences, (long long)kv.kv_heads);
+        return t;
+    }
+    // the caller's scratch, or `bytes` of new one
+    at::Tensor scratch(PyObject* given, size_t* bytes) const {
+        if (given == Py_None) return at::empty({(int64_t)*bytes}, at::TensorOptions().dtype(at::kByte).device(x.device()));
+        const at::Tensor& t = here(tensor(given, "workspace"), "workspace");
+        *bytes = (size_t)t.numel() * t.element_size();
+        return t;
+    }
+};
+
+// What both appends take: the rows, their heads, the angles
+struct Append {
+    bitnet_dtype dt;
+    const at::Tensor& qkv;
+    int64_t T, heads, D, rotary = 0;
+    Cache c;
+    const float* freq = nullptr;
+    static int64_t head_dim(const at::Tensor& qkv, PyObject* ok, int64_t heads) {
+        const at::Tensor& k = tensor(ok, "k_cache");
+        const int64_t kv_heads = k.dim() == 6 ? k.size(1) : 1;
+        if (heads <= 0 || heads > qkv.size(1) || qkv.size(1) % (heads + 2 * kv_heads) != 0)
+            raise(PyExc_ValueError, "qkv must have the columns of heads queries and two times kv heads keys and values");
+        return qkv.size(1) / (heads + 2 * kv_heads);
+    }
+    Append(PyObject* oqkv, PyObject* ofreq, PyObject* ok, PyObject* ov, PyObject* otable, PyObject* olen, PyObject* oheads, PyObject* ostart)
+        : qkv(matrix(oqkv, "qkv", &dt)), T(qkv.size(0)), heads(integer(oheads)), D(head_dim(qkv, ok, heads)), c(qkv, D, ok, ov, otable, olen, ostart) {
+        if (ofreq == Py_None) return;
+        const at::Tensor& f = c.here(ofreq, "inv_freq", at::kFloat);
+        if (f.dim() != 1) raise(PyExc_ValueError, "inv_freq must be 1-D");
+        freq = static_cast<const float*>(f.const_data_ptr());
+        rotary = 2 * f.size(0);
+    }
 };
 
 ENTRY(rope_kv_append) {      // qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_start, pairs, q
     return entry(n, 10, [&] {
-        bitnet_dtype dt;
-        const at::Tensor& qkv = matrix(a[0], "qkv", &dt);
-        const int64_t T = qkv.size(0), heads = integer(a[6]);
-        const at::Tensor& k = tensor(a[2], "k_cache");
-        const int64_t kv_heads = k.dim() == 6 ? k.size(1) : 1;
-        if (heads <= 0 || heads > qkv.size(1) || qkv.size(1) % (heads + 2 * kv_heads) != 0)
-            raise(PyExc_ValueError, "qkv must have the columns of heads queries and two times kv heads keys and values");
-        const int64_t D = qkv.size(1) / (heads + 2 * kv_heads);
-        Cache c(qkv, D, a[2], a[3], a[4], a[5], a[7]);
-        const float* freq = nullptr;
-        int64_t rotary = 0;
-        if (a[1] != Py_None) {
-            const at::Tensor& f = c.here(a[1], "inv_freq", at::kFloat);
-            if (f.dim() != 1) raise(PyExc_ValueError, "inv_freq must be 1-D");
-            freq = static_cast<const float*>(f.const_data_ptr());
-            rotary = 2 * f.size(0);
-        }
+        Append p(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]);
         const int pairs = truth(a[8]) ? 1 : 0;
-        at::Tensor q = c.output(a[9], "q", {T, heads, D}, at::kBFloat16);
-        const void* xp = qkv.const_data_ptr();
-        void *qp = q.mutable_data_ptr(), *st = c.stream();
-        call("bitnet_rope_kv_append", [&] { return abi.rope_kv_append(xp, dt, freq, rotary, pairs, &c.kv, T, heads, qp, st); });
+        at::Tensor q = p.c.output(a[9], "q", {p.T, p.heads, p.D}, at::kBFloat16);
+        const void* xp = p.qkv.const_data_ptr();
+        void *qp = q.mutable_data_ptr(), *st = p.c.stream();
+        call("bitnet_rope_kv_append", [&] { return abi.rope_kv_append(xp, p.dt, p.freq, p.rotary, pairs, &p.c.kv, p.T, p.heads, qp, st); });
+        return THPVariable_Wrap(q);
+    });
+}
+
+ENTRY(norm_rope_kv_append) {      // qkv, inv_freq, k_cache, v_cache, page_table, kv_len, heads, q_gain, k_gain, eps, q_start, pairs, norm, shift, q
+    return entry(n, 15, [&] {
+        Append p(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[10]);
+        const float *qg = p.c.list<float>(a[7], "q_gain", at::kFloat, p.D, true), *kg = p.c.list<float>(a[8], "k_gain", at::kFloat, p.D, true);
+        const float eps = real(a[9]);
+        const int pairs = truth(a[11]) ? 1 : 0, norm = truth(a[12]) ? 1 : 0;
+        const int32_t* shift = p.c.list<int32_t>(a[13], "shift", at::kInt, p.c.kv.sequences, true);
+        at::Tensor q = p.c.output(a[14], "q", {p.T, p.heads, p.D}, at::kBFloat16);
+        const void* xp = p.qkv.const_data_ptr();
+        void *qp = q.mutable_data_ptr(), *st = p.c.stream();
+        call("bitnet_norm_rope_kv_append",
+             [&] { return abi.norm_rope_kv_append(xp, p.dt, norm, qg, kg, eps, p.freq, p.rotary, pairs, shift, &p.c.kv, p.T, p.heads, qp, st); });
         return THPVariable_Wrap(q);
     });
 }
@@ -485,6 +539,109 @@ PyObject* attention(PyObject* const* a, bool prefill) {      // q, k_cache, v_ca
 ENTRY(attention_decode) { return entry(n, 10, [&] { return attention(a, false); }); }
 ENTRY(attention_prefill) { return entry(n, 10, [&] { return attention(a, true); }); }
 
+// The rows of attention that is more than its output: q [T, heads, D], the cache, scale, the output
+struct Rows {
+    const at::Tensor& q;
+    int64_t T, heads, D;
+    Cache c;
+    float scale;
+    at::ScalarType dt;
+    at::Tensor y;
+    static const at::Tensor& checked(PyObject* o) {
+        const at::Tensor& q = tensor(o, "q", at::kBFloat16);
+        if (q.dim() != 3) raise(PyExc_ValueError, "q must be 3-D");
+        return q;
+    }
+    Rows(PyObject* oq, PyObject* ok, PyObject* ov, PyObject* otable, PyObject* olen, PyObject* ostart, PyObject* oscale, PyObject* otype, PyObject* oy)
+        : q(checked(oq)), T(q.size(0)), heads(q.size(1)), D(q.size(2)), c(q, D, ok, ov, otable, olen, ostart) {
+        if (ostart == Py_None && T != c.kv.sequences) raise(PyExc_ValueError, "q must have one row per row of page_table");
+        if (D <= 0) raise(PyExc_ValueError, "q has heads of no dims");
+        scale = oscale == Py_None ? (float)(1.0 / std::sqrt((double)D)) : real(oscale);
+        dt = out_type(otype);
+        if (dt == at::kInt) raise(PyExc_ValueError, "y_dtype must be F32 or BF16");
+        y = c.output(oy, "y", {T, heads * D}, dt);
+    }
+    bitnet_dtype type() const { return dt == at::kFloat ? BITNET_F32 : BITNET_BF16; }
+};
+
+ENTRY(attention_decode_shared) {      // q, k_cache, v_cache, page_table, kv_len, prefix_start, prefix_len, scale, y_dtype, y, workspace
+    return entry(n, 11, [&] {
+        Rows r(a[0], a[1], a[2], a[3], a[4], Py_None, a[7], a[8], a[9]);
+        const at::Tensor& len = r.c.here(a[6], "prefix_len", at::kInt);
+        if (len.dim() != 1) raise(PyExc_ValueError, "prefix_len must be 1-D");
+        const int64_t groups = len.size(0);
+        const int32_t* start = r.c.list<int32_t>(a[5], "prefix_start", at::kInt, groups + 1, false);
+        size_t bytes = 0;
+        if (a[10] == Py_None)
+            call("bitnet_attention_shared_workspace", [&] { return abi.attention_shared_workspace(&r.c.kv, groups, r.heads, &bytes); });
+        at::Tensor ws = r.c.scratch(a[10], &bytes);
+        const void* qp = r.q.const_data_ptr();
+        const int32_t* lp = static_cast<const int32_t*>(len.const_data_ptr());
+        void *wp = ws.mutable_data_ptr(), *yp = r.y.mutable_data_ptr(), *st = r.c.stream();
+        call("bitnet_attention_decode_shared",
+             [&] { return abi.attention_decode_shared(qp, &r.c.kv, start, lp, groups, r.heads, r.scale, yp, r.type(), wp, bytes, st); });
+        return THPVariable_Wrap(r.y);
+    });
+}
+
+PyObject* attention_weights(PyObject* const* a, bool prefill) {      // q, k_cache, v_cache, page_table, kv_len, q_start, weights, scale, y_dtype, y, workspace
+    Rows r(a[0], a[1], a[2], a[3], a[4], a[5], a[7], a[8], a[9]);
+    if (prefill && a[5] == Py_None) raise(PyExc_TypeError, "q_start must be a CUDA/HIP tensor");
+    const at::Tensor& w = r.c.weights(a[6], "weights");
+    size_t bytes = 0;
+    if (a[10] == Py_None)
+        call("bitnet_attention_weights_workspace", [&] { return abi.attention_weights_workspace(&r.c.kv, r.T, r.heads, prefill, r.type(), &bytes); });
+    at::Tensor ws = r.c.scratch(a[10], &bytes);
+    const void* qp = r.q.const_data_ptr();
+    float* weights = static_cast<float*>(w.mutable_data_ptr());
+    const int64_t stride = w.size(2);
+    void *wp = ws.mutable_data_ptr(), *yp = r.y.mutable_data_ptr(), *st = r.c.stream();
+    if (prefill)
+        call("bitnet_attention_prefill_weights",
+             [&] { return abi.attention_prefill_weights(qp, &r.c.kv, r.T, r.heads, r.scale, yp, r.type(), weights, stride, wp, bytes, st); });
+    else
+        call("bitnet_attention_decode_weights",
+             [&] { return abi.attention_decode_weights(qp, &r.c.kv, r.heads, r.scale, yp, r.type(), weights, stride, wp, bytes, st); });
+    return THPVariable_Wrap(r.y);
+}
+ENTRY(attention_decode_weights) { return entry(n, 11, [&] { return attention_weights(a, false); }); }
+ENTRY(attention_prefill_weights) { return entry(n, 11, [&] { return attention_weights(a, true); }); }
+
+ENTRY(kv_evict) {      // k_cache, v_cache, page_table, kv_len, weights, keep, recent, page_table_out, kv_len_out, weights_out, kept
+    return entry(n, 11, [&] {
+        const at::Tensor& k = tensor(a[0], "k_cache", at::kBFloat16);
+        Cache c(k, k.dim() == 6 ? k.size(3) * 8 : 8, a[0], a[1], a[2], a[3], Py_None);
+        const at::Tensor& w = c.weights(a[4], "weights");
+        const int64_t keep = integer(a[5]), recent = integer(a[6]), B = c.kv.sequences;
+        if (!THPVariable_Check(a[7]) || !THPVariable_Unpack(a[7]).is_cuda()) raise(PyExc_TypeError, "page_table_out must be a CUDA/HIP tensor");
+        const at::Tensor& table = c.here(THPVariable_Unpack(a[7]), "page_table_out");
+        if (table.scalar_type() != at::kInt) raise(PyExc_TypeError, "page_table_out has dtype %s", dtype_name(table.scalar_type()));
+        two_d(table, "page_table_out");
+        const int64_t pages = table.size(1);
+        if (table.size(0) != B) raise(PyExc_ValueError, "page_table_out must have a row per row of page_table");
+        if ((pages > 1 && table.stride(1) != 1) || (B > 1 && table.stride(0) < pages)) raise(PyExc_ValueError, "page_table_out must have contiguous rows");
+        const int64_t most = std::min(keep, c.kv.max_pages * c.kv.page_tokens);
+        if (keep <= 0 || pages * c.kv.page_tokens < most) raise(PyExc_ValueError, "page_table_out must have room for keep tokens, of which there is one at least");
+        at::Tensor len = c.output(a[8], "kv_len_out", {B}, at::kInt);
+        at::Tensor out = a[9] == Py_None ? at::empty({B, c.kv.kv_heads, pages * c.kv.page_tokens}, at::TensorOptions().dtype(at::kFloat).device(k.device()))
+                                         : c.weights(a[9], "weights_out");
+        at::Tensor kept = c.output(a[10], "kept", {B, c.kv.kv_heads, keep}, at::kInt);
+        const float* wp = static_cast<const float*>(w.const_data_ptr());
+        const int32_t* tp = static_cast<const int32_t*>(table.const_data_ptr());
+        float* op = static_cast<float*>(out.mutable_data_ptr());
+        int32_t *lp = static_cast<int32_t*>(len.mutable_data_ptr()), *kp = static_cast<int32_t*>(kept.mutable_data_ptr());
+        void* st = c.stream();
+        const int64_t stride = w.size(2), stride_out = out.size(2), table_stride = B > 1 ? table.stride(0) : pages;
+        call("bitnet_kv_evict", [&] { return abi.kv_evict(&c.kv, wp, stride, keep, recent, tp, table_stride, op, stride_out, lp, kp, st); });
+        PyObject* got = PyTuple_New(3);
+        if (!got) throw Raised();
+        PyTuple_SET_ITEM(got, 0, THPVariable_Wrap(len));
+        PyTuple_SET_ITEM(got, 1, THPVariable_Wrap(out));
+        PyTuple_SET_ITEM(got, 2, THPVariable_Wrap(kept));
+        return got;
+    });
+}
+
 // bind({name: address}, BitnetError)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *addresses, *cls;
@@ -504,6 +661,8 @@ PyObject* bind(PyObject*, PyObject* args) {
     TAKE(linear_ws); TAKE(linear_fused); TAKE(linear_fused_segmented); TAKE(rmsnorm_linear_fused);
     TAKE(rmsnorm_linear_fused_segmented); TAKE(swiglu_linear_fused); TAKE(ffn_gate_up_fused);
     TAKE(rope_kv_append); TAKE(attention_workspace); TAKE(attention_decode); TAKE(attention_prefill);
+    TAKE(norm_rope_kv_append); TAKE(attention_shared_workspace); TAKE(attention_decode_shared); TAKE(attention_weights_workspace);
+    TAKE(attention_decode_weights); TAKE(attention_prefill_weights); TAKE(kv_evict);
 #undef TAKE
     abi = got;
     Py_INCREF(cls);
@@ -518,6 +677,7 @@ PyMethodDef methods[] = {
     FAST(quantize_acts), FAST(rmsnorm_quantize), FAST(swiglu_quantize), FAST(linear), FAST(linear_segmented), FAST(linear_ws),
     FAST(linear_fused), FAST(rmsnorm_linear_fused), FAST(swiglu_linear_fused), FAST(ffn_gate_up_fused),
     FAST(rope_kv_append), FAST(attention_decode), FAST(attention_prefill),
+    FAST(norm_rope_kv_append), FAST(attention_decode_shared), FAST(attention_decode_weights), FAST(attention_prefill_weights), FAST(kv_evict),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

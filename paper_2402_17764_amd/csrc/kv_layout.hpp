@@ -80,4 +80,28 @@ BITNET_BOTH inline int64_t tiles_at_most(int64_t T, int64_t B, int each, int siz
     return extra == 1 ? (T * each + size - 1) / size + B - 1 : T * each / size + extra * B;
 }
 
+// Runs of sequences that have their first tokens in common: group i's are start[i] ... start[i + 1] - 1 of them, and share len[i] tokens.
+struct Prefixes {
+    const int32_t *start, *len;
+    int32_t groups;
+};
+// The sequences [first, first + n) of a group, and how many tokens they share.
+struct SharedRows {
+    int first, n, len;
+    BITNET_BOTH SharedRows(const KvView& kv, const Prefixes& p, int i) {
+        const int s = p.start[i], e = p.start[i + 1];
+        first = s < 0 ? 0 : s > kv.B ? kv.B : s;
+        n = (e < first ? first : e > kv.B ? kv.B : e) - first;
+        len = kv.length(p.len[i]);
+    }
+};
+// of the `len` tokens of sequence b, those that it shares
+BITNET_BOTH inline int shared_tokens(const KvView& kv, const Prefixes& p, int b, int len) {
+    const SharedRows r(kv, p, sequence_of_tile(p.start, p.groups, b, 1, 1, 0));
+    return b < r.first || b >= r.first + r.n ? 0 : len < r.len ? len : r.len;
+}
+// of a sequence's blocks those that hold tokens of its own, behind `shared` ones: the first, and their number
+BITNET_BOTH inline int own_first(int shared) { return shared / kKvBlock; }
+BITNET_BOTH inline int own_blocks(int len, int shared) { return shared >= len ? 0 : (len + kKvBlock - 1) / kKvBlock - own_first(shared); }
+
 }  // namespace bitnet
