@@ -83,70 +83,202 @@ struct ColumnArgs {
     const uint16_t* q;
     const float* state;                // [T][heads][2]: m, l
     float* weights;                    // [B][kv heads][stride]
-    int64_t stride, tasks;             // of the weights: sequences times kv heads times tiles of keys
+    float* parts;                      // [tasks][keys of a tile]
+    int64_t stride, tasks;             // of the weights: tiles of keys times splits times sequences times kv heads
     float scale;
-    int heads, group, T, tiles;
+    int heads, group, T;
+    int splits, least;                 // workgroups that share a tile's rows, at most, and stages that one has at least
+    uint32_t magic, shift;             // of the division by `group`: the quotient of n is (high word of n magic + n) >> shift, n below 2^31
+    __device__ int token(int row) const { return (int)((__umulhi((uint32_t)row, magic) + (uint32_t)row) >> shift); }
 };
 
-// A workgroup takes a tile of keys of one sequence and key-value head, 32 kKB for each of its four waves, in registers, and goes through the rows that
-// see any of them, 16 at a time: scores are products of keys (down) and queries (across), so that a lane sums up eight tokens for its
-// queries, and the 16 lanes of a group meet at the end.
-template <int kC, bool kExact, int kKB>
+// The shape of a workgroup: four waves of 32 kKB keys each, in registers, and stages of 16 kTiles rows in LDS.
+template <int kC> struct Columns {
+    static constexpr int kKB = kC <= 4 ? 2 : 1, kKeys = 128 * kKB, kTiles = kC <= 4 ? 4 : 2, kRows = 16 * kTiles;
+};
+
+// What a tile of keys is: its sequence and head, the rows that see any of it, and how they are shared out, in stages.
+template <int kC>
+struct ColumnTile {
+    int h, b, share, tile, blocks, blk, j0, rows, first, stages, run;
+    NewTokens nt;
+    // Heads side by side, so that with a multiple of eight of them a head's tiles meet on one XCD, whose L2 holds its queries; the first tiles, which most
+    // rows see, first with all their shares, so that what comes last is short.
+    __device__ ColumnTile(const ColumnArgs& a, const KvView& kv, int64_t task)
+        : h((int)(task % kv.kv_heads)), b((int)(task / kv.kv_heads % kv.B)), share((int)(task / kv.kv_heads / kv.B % a.splits)),
+          tile((int)(task / kv.kv_heads / kv.B / a.splits)), nt(kv, b, a.T) {
+        blocks = blocks_of(kv, b);
+        blk = tile * (4 * Columns<kC>::kKB);
+        j0 = blk * kKvBlock;
+        rows = nt.n * a.group;
+        if (nt.n == 0 || blk >= blocks) { stages = 0, run = 1, first = 0; return; }
+        first = max(j0 - nt.pos0, 0) * a.group / 16 * 16;
+        stages = (rows - first + Columns<kC>::kRows - 1) / Columns<kC>::kRows;
+        run = max((stages + a.splits - 1) / a.splits, a.least);
+    }
+};
+
+// dims d0 ... d0 + 7 of a row, zeros behind its end; settle_dims once they are there
+__device__ inline v4u load_dims(const uint16_t* row, int d0, int D) {
+    v4u w = {0, 0, 0, 0};
+    if (D >= 8) {
+        __builtin_memcpy(&w, row + min(d0, D - 8), 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (d0 + 2 * i < D) {
+                uint32_t two;
+                __builtin_memcpy(&two, row + d0 + 2 * i, 4);
+                w[i] = two;
+            }
+    }
+    return w;
+}
+__device__ inline v4u settle_dims(v4u w, int d0, int D) {
+    if (D < 8) return w;
+    const int over = max(d0 + 8 - D, 0) >> 1;
+    if (over & 1) w = (v4u){w[1], w[2], w[3], 0};
+    if (over & 2) w = (v4u){w[2], w[3], 0, 0};
+    if (over >= 4) w = (v4u){0, 0, 0, 0};
+    return w;
+}
+
+// A workgroup takes a tile of keys and a run of the rows that see any of it, which come through LDS a stage at a time for its four waves, the next
+// stage requested while one is worked on.  Scores are products of keys (down) and queries (across), so that a lane sums up eight tokens of a block for
+// its queries; the lanes of a group meet at the end.
+template <int kC, bool kExact>
 __global__ __launch_bounds__(256, 2) void attention_weights_of_runs(ColumnArgs a, KvView kv) {
+    using Shape = Columns<kC>;
+    constexpr int kKB = Shape::kKB, kTiles = Shape::kTiles, kRows = Shape::kRows, kPieces = kTiles * kC / 4;
+    __shared__ uint4 queries[2][kTiles * kC * 64];
+    __shared__ float2 stats[2][kRows];                      // m times scale, or 0, and 1 / l, or 0
+    __shared__ int positions[2][kRows];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int D = kExact ? 32 * kC : kv.D, Dp = kv_padded_dim(D), quads = Dp >> 3;
+    // this wave's share of a stage: kPieces chunks of 32 dims, from c0 on, of the rows of one tile
+    const int my_tile = wave * kTiles / 4, c0 = kTiles == 4 ? 0 : (wave & 1) * (kC / 2);
     for (int64_t task = blockIdx.x; task < a.tasks; task += gridDim.x) {
-        // heads side by side, so that with a multiple of eight of them a head's tiles meet on one XCD, whose L2 holds its queries
-        const int h = (int)(task % kv.kv_heads);
-        const int64_t rest = task / kv.kv_heads;
-        const int tile = (int)(rest % a.tiles), b = (int)(rest / a.tiles);
-        const NewTokens nt(kv, b, a.T);
-        const int len = kv.length(kv.kv_len[b]), blocks = (len + kKvBlock - 1) / kKvBlock, blk = (tile * 4 + wave) * kKB, j0 = blk * kKvBlock;
-        if (nt.n == 0 || blk >= blocks) continue;
+        const ColumnTile<kC> t(a, kv, task);
+        const int s0 = t.share * t.run, s1 = min(s0 + t.run, t.stages);
+        if (s0 >= s1) continue;                             // the same for all waves
+        struct { v4u w[kPieces]; float m, l; int pos; bool there; } next;
+        auto load = [&](int s) {
+            const int R = t.first + s * kRows + my_tile * 16 + r, tok = a.token(R), row = (t.nt.first + tok) * a.heads + t.h * a.group + R - tok * a.group;
+            const bool there = R < t.rows;
+            const uint16_t* from = a.q + (int64_t)(there ? row : 0) * D;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int d0 = 32 * (c0 + i) + 8 * g;
+                if (kExact) __builtin_memcpy(&next.w[i], from + d0, 16);
+                else next.w[i] = load_dims(from, d0, D);
+            }
+            next.m = kMinusInf, next.l = 0.0f;
+            if (there) {
+                next.m = a.state[2 * (int64_t)row];
+                next.l = a.state[2 * (int64_t)row + 1];
+            }
+            next.pos = there ? t.nt.pos0 + tok : -1;
+            next.there = there;
+        };
+        auto publish = [&](int s) {                         // rows that there are not are zeros, and their l is 0
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                v4u w = kExact ? next.w[i] : settle_dims(next.w[i], 32 * (c0 + i) + 8 * g, D);
+                if (!next.there) w = (v4u){0, 0, 0, 0};
+                queries[s & 1][(my_tile * kC + c0 + i) * 64 + lane] = __builtin_bit_cast(uint4, w);
+            }
+            if (c0 == 0 && g == 0) {
+                stats[s & 1][my_tile * 16 + r] = {next.m == kMinusInf ? 0.0f : next.m * a.scale, next.l > 0.0f ? 1.0f / next.l : 0.0f};
+                positions[s & 1][my_tile * 16 + r] = next.pos;
+            }
+        };
+        load(s0);
+        const int blk = t.blk + wave * kKB, j0 = blk * kKvBlock;
         v8bf k[kKB][kC][2];
         bool known[kKB];
 #pragma unroll
         for (int u = 0; u < kKB; ++u) {
-            const int number = blk + u < blocks ? kv.block(kv.table + b * kv.table_stride, blk + u, h) : -1;
+            const int number = blk + u < t.blocks ? kv.block(kv.table + t.b * kv.table_stride, blk + u, t.h) : -1;
             known[u] = number >= 0;
             const char* from = reinterpret_cast<const char*>(kv.k) + (int64_t)max(number, 0) * kKvBlock * Dp * 2;
 #pragma unroll
             for (int c = 0; c < kC; ++c)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int off = (kExact || c < whole_chunks(kC) ? 4 * c + g : min(4 * c + g, quads - 1)) * 512 + r * 16 + 256 * t;
-                    k[u][c][t] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4u*>(from + off));
+                for (int i = 0; i < 2; ++i) {
+                    const int off = (kExact || c < whole_chunks(kC) ? 4 * c + g : min(4 * c + g, quads - 1)) * 512 + r * 16 + 256 * i;
+                    k[u][c][i] = __builtin_bit_cast(v8bf, *reinterpret_cast<const v4u*>(from + off));
                 }
         }
         float acc[kKB][8] = {};
-        const int rows = nt.n * a.group, tok0 = max(j0 - nt.pos0, 0);
-        for (int R0 = tok0 * a.group / 16 * 16; R0 < rows; R0 += 16) {
-            const int R = R0 + r, tok = token_of(R, a.group), row = R < rows ? (nt.first + tok) * a.heads + h * a.group + R - tok * a.group : -1;
-            const int pos = row >= 0 ? nt.pos0 + tok : -1;
-            v8bf qf[kC];
-            load_query<kC, kExact>(qf, row >= 0 ? a.q + (int64_t)row * D : nullptr, g, D);
-            float m = kMinusInf, l = 0.0f;
-            if (row >= 0) {
-                m = a.state[2 * (int64_t)row];
-                l = a.state[2 * (int64_t)row + 1];
+        // Scores of 16 rows against the wave's keys, and what becomes of them.  The matrix instructions of a tile of rows run beside the exponentials of
+        // the one in front of it, where the source puts them so: one after each, with a fence behind.
+        struct Scores { v4f x[kKB][2]; float2 st; };
+        auto weight = [&](const Scores& y, int u, int j) { return exp2_fast(__builtin_fmaf(y.x[u][j >> 2][j & 3], a.scale, -y.st.x)); };
+        auto scores = [&](auto with, Scores& x, const v8bf (&q)[kC], const Scores& old) {
+#pragma unroll
+            for (int i = 0; i < 2 * kC * kKB; ++i) {
+                const int c = i / (2 * kKB), u = i / 2 % kKB, e = i % 2;
+                x.x[u][e] = mfma_bf16(k[u][c][e], q[c], c ? x.x[u][e] : (v4f){0, 0, 0, 0});
+#pragma unroll
+                for (int w = 0; w < 8 * kKB; ++w)
+                    if (decltype(with)::value && w * kC / 4 == i) acc[w / 8][w % 8] = __builtin_fmaf(weight(old, w / 8, w % 8), old.st.y, acc[w / 8][w % 8]);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            settle_query<kC, kExact>(qf, g, D);
-            const float base = m == kMinusInf ? 0.0f : m * a.scale, inv = l > 0.0f ? 1.0f / l : 0.0f;
-            v4f s[kKB][2] = {};
+        };
+        auto flush = [&](const Scores& y) {
 #pragma unroll
             for (int u = 0; u < kKB; ++u)
 #pragma unroll
-                for (int c = 0; c < kC; ++c)
+                for (int j = 0; j < 8; ++j) acc[u][j] = __builtin_fmaf(weight(y, u, j), y.st.y, acc[u][j]);
+        };
+        publish(s0);
+        __builtin_amdgcn_s_waitcnt(0);                      // the keys: waited for in the loop, they would be the next stage's loads too
+        for (int s = s0; s < s1; ++s) {
+            __syncthreads();
+            if (s + 1 < s1) load(s + 1);
+            // positions do not fall: the first row's says whether all see all of the wave's keys
+            if (__builtin_amdgcn_readfirstlane(positions[s & 1][0]) >= j0 + kKvBlock * kKB - 1) {
+                v8bf q[2][kC];
+                Scores x[2];
+                auto read = [&](int i) {
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) s[u][t] = mfma_bf16(k[u][c][t], qf[c], s[u][t]);
+                    for (int c = 0; c < kC; ++c) q[i & 1][c] = __builtin_bit_cast(v8bf, queries[s & 1][(i * kC + c) * 64 + lane]);
+                    x[i & 1].st = stats[s & 1][i * 16 + r];
+                };
+                read(0);
 #pragma unroll
-            for (int u = 0; u < kKB; ++u)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float p = exp2_fast(__builtin_fmaf(s[u][j >> 2][j & 3], a.scale, -base));
-                    if (known[u] && j0 + u * kKvBlock + 8 * g + j <= pos) acc[u][j] = __builtin_fmaf(p, inv, acc[u][j]);
+                for (int i = 0; i < kTiles; ++i) {
+                    if (i == 0) scores(std::false_type(), x[0], q[0], x[0]);
+                    else scores(std::true_type(), x[i & 1], q[i & 1], x[1 - (i & 1)]);
+                    if (i + 1 < kTiles) read(i + 1);
                 }
+                flush(x[(kTiles - 1) & 1]);
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < kTiles; ++i) {
+                    const int pos = positions[s & 1][i * 16 + r];
+                    if (!__builtin_amdgcn_ballot_w64(pos >= j0)) continue;
+                    v8bf q[kC];
+#pragma unroll
+                    for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(v8bf, queries[s & 1][(i * kC + c) * 64 + lane]);
+                    Scores x;
+                    x.st = stats[s & 1][i * 16 + r];
+                    scores(std::false_type(), x, q, x);
+#pragma unroll
+                    for (int u = 0; u < kKB; ++u)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float p = j0 + u * kKvBlock + 8 * g + j <= pos ? weight(x, u, j) : 0.0f;
+                            acc[u][j] = __builtin_fmaf(p, x.st.y, acc[u][j]);
+                        }
+                }
+            }
+            if (s + 1 < s1) publish(s + 1);                 // the other half, which all waves left at the barrier
         }
+        const bool whole = t.run >= t.stages;
+        const int len = kv.length(kv.kv_len[t.b]);
+        float* to = a.weights + ((int64_t)t.b * kv.kv_heads + t.h) * a.stride;
+        float* part = a.parts + task * Shape::kKeys - t.j0;
 #pragma unroll
         for (int u = 0; u < kKB; ++u)
 #pragma unroll
@@ -156,13 +288,48 @@ __global__ __launch_bounds__(256, 2) void attention_weights_of_runs(ColumnArgs a
                 v += dpp_f32<0x4E>(v);
                 v += dpp_f32<0x141>(v);
                 v += dpp_f32<0x140>(v);
+                v = known[u] ? v : 0.0f;
                 const int at = j0 + u * kKvBlock + 8 * g + j;
-                if (r == j && at < len) {
-                    float* to = a.weights + ((int64_t)b * kv.kv_heads + h) * a.stride + at;
-                    *to = (at >= nt.pos0 ? 0.0f : *to) + v;           // the call's own tokens begin with nothing
-                }
+                if (r != j || at >= len) continue;
+                if (whole) to[at] = (at >= t.nt.pos0 ? 0.0f : to[at]) + v;       // the call's own tokens begin with nothing
+                else part[at] = v;
             }
+        __syncthreads();
     }
+}
+
+// The parts of tiles whose rows several workgroups shared, added up.
+template <int kC>
+__global__ __launch_bounds__(Columns<kC>::kKeys) void attention_weights_join(ColumnArgs a, KvView kv) {
+    for (int64_t task = blockIdx.x; task < a.tasks; task += gridDim.x) {
+        const ColumnTile<kC> t(a, kv, task);
+        const int at = t.j0 + (int)threadIdx.x;
+        if (t.share > 0 || t.run >= t.stages || at >= kv.length(kv.kv_len[t.b])) continue;
+        const int64_t pitch = (int64_t)kv.B * kv.kv_heads * Columns<kC>::kKeys;
+        const float* part = a.parts + task * Columns<kC>::kKeys + threadIdx.x;
+        float sum = 0.0f;
+        for (int s = 0; s * t.run < t.stages; ++s) sum += part[s * pitch];
+        float* to = a.weights + ((int64_t)t.b * kv.kv_heads + t.h) * a.stride + at;
+        *to = (at >= t.nt.pos0 ? 0.0f : *to) + sum;
+    }
+}
+
+// How many workgroups share the rows of a tile of keys: as many as make 1024 of them, two rounds of what the chip holds, with two stages or more each;
+// their sums go through the workspace and another launch (us without that launch, 1 / 2 / 4 / 8 / 16 / 32: 64 heads over 8, 512 tokens 110 / 70 / 37 / 21 / 13 /
+// 8.8, 2048 tokens 351 / 192 / 112 / 81 / 73 / -; 40 heads, 2048 tokens 57 / 46 / 49 / 50 / 57 / -; six of 450 behind 250, 32 heads of 100 36 / 38 / 42 / 54 / 66 / -).
+struct ColumnsPlan {
+    int64_t tasks;
+    int splits;
+    size_t bytes;
+};
+constexpr int kLeastStages = 2;
+template <int kC>
+ColumnsPlan columns_plan(const KvView& kv, int64_t T, int group) {
+    using Shape = Columns<kC>;
+    const int64_t tiles = (int64_t)kv.B * kv.kv_heads * ceil_div(kv.max_blocks, 4 * Shape::kKB), most = ceil_div(T * group, Shape::kRows * kLeastStages);
+    int64_t n = tiles < 1024 ? 1024 / tiles : 1;
+    n = n < most ? n : most;
+    return {tiles * n, (int)n, n < 2 ? 0 : (size_t)(tiles * n * Shape::kKeys) * 4};
 }
 
 // Splits of single tokens' rows and the workspace: parts, then scores.
@@ -179,8 +346,22 @@ constexpr int64_t kMostBlocks = 1 << 20;                   // of a launch that l
 
 }  // namespace
 
+// Of runs: the rows' states, the parts of tiles of keys, and what the attention takes.
+struct RunsPlan { size_t states, parts, attention; };
+static RunsPlan runs_plan(const KvView& kv, int64_t T, int heads, bool f32) {
+    RunsPlan p{((size_t)(T * heads) * 8 + 15) / 16 * 16, 0, attention_prefill_kept_bytes(kv, T, heads, f32)};
+    (void)for_head_size(kv.D, [&](auto c, auto, auto) {
+        p.parts = columns_plan<c.value>(kv, T, heads / kv.kv_heads).bytes;
+        return hipSuccess;
+    });
+    return p;
+}
+
 size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill, bool f32) {
-    if (prefill) return ((size_t)(T * heads) * 8 + 15) / 16 * 16 + attention_prefill_kept_bytes(kv, T, heads, f32);
+    if (prefill) {
+        const RunsPlan p = runs_plan(kv, T, heads, f32);
+        return p.states + p.parts + p.attention;
+    }
     const TokensPlan p = tokens_plan(kv, heads);
     return p.parts + p.scores;
 }
@@ -213,17 +394,24 @@ hipError_t launch_attention_decode_weights(const void* q, const KvView& kv, int 
 
 hipError_t launch_attention_prefill_weights(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, float* weights, int64_t stride,
                                             void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    const size_t states = ((size_t)(T * heads) * 8 + 15) / 16 * 16;
+    const RunsPlan plan = runs_plan(kv, T, heads, f32);
+    char* at = static_cast<char*>(workspace);
     KeptRows keep;
-    keep.state = static_cast<float*>(workspace);
-    const hipError_t e = launch_attention_prefill_kept(q, kv, T, heads, scale, o, f32, keep, static_cast<char*>(workspace) + states, workspace_bytes - states, stream);
+    keep.state = reinterpret_cast<float*>(at);
+    const hipError_t e = launch_attention_prefill_kept(q, kv, T, heads, scale, o, f32, keep, at + plan.states + plan.parts, workspace_bytes - plan.states - plan.parts, stream);
     if (e != hipSuccess) return e;
     return for_head_size(kv.D, [&](auto c, auto, auto exact) {
-        constexpr int kKB = c.value <= 4 ? 2 : 1;
-        const int tiles = (int)ceil_div(kv.max_blocks, 4 * kKB);
-        const int64_t tasks = (int64_t)kv.B * kv.kv_heads * tiles;
-        const ColumnArgs a{static_cast<const uint16_t*>(q), keep.state, weights, stride, tasks, scale * 1.44269504f, heads, heads / kv.kv_heads, (int)T, tiles};
-        attention_weights_of_runs<c.value, exact.value, kKB><<<(unsigned)(tasks < kMostBlocks ? tasks : kMostBlocks), 256, 0, stream>>>(a, kv);
+        const int group = heads / kv.kv_heads;
+        const ColumnsPlan p = columns_plan<c.value>(kv, T, group);
+        int shift = 0;
+        while ((1 << shift) < group) ++shift;
+        const ColumnArgs a{static_cast<const uint16_t*>(q), keep.state, weights, reinterpret_cast<float*>(at + plan.states), stride, p.tasks, scale * 1.44269504f,
+                           heads, group, (int)T, p.splits, kLeastStages, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - group)) / group + 1), (uint32_t)shift};
+        const unsigned blocks = (unsigned)(p.tasks < kMostBlocks ? p.tasks : kMostBlocks);
+        attention_weights_of_runs<c.value, exact.value><<<blocks, 256, 0, stream>>>(a, kv);
+        const hipError_t ran = hipGetLastError();
+        if (ran != hipSuccess || p.splits < 2) return ran;
+        attention_weights_join<c.value><<<blocks, Columns<c.value>::kKeys, 0, stream>>>(a, kv);
         return hipGetLastError();
     });
 }
