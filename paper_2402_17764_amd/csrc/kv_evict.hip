@@ -25,10 +25,11 @@ __device__ inline uint32_t rank_of(float w) {
     const uint32_t u = __float_as_uint(w + 0.0f);
     return w != w ? 0xFFFFFFFFu : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ inline float weight_of(uint32_t rank) { return __uint_as_float(rank & 0x80000000u ? rank == 0xFFFFFFFFu ? 0x7FC00000u : rank & 0x7FFFFFFFu : ~rank); }
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kEach = 4;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kEach = 4, kTurn = kThreads * kEach;
 
-// the sum over the lanes in front of this one, of two counts in one word
+// the sum over the lanes in front of this one
 __device__ inline uint32_t wave_before(uint32_t v, uint32_t* all) {
     const int lane = threadIdx.x & 63;
     uint32_t s = v;
@@ -40,87 +41,153 @@ __device__ inline uint32_t wave_before(uint32_t v, uint32_t* all) {
     *all = __shfl(s, 63);
     return s - v;
 }
+// n plus the number of lanes in front of this one whose bit is set
+__device__ inline uint32_t lanes_before(uint64_t bits, uint32_t n) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, n));
+}
 
+// kTurns turns of kTurn tokens stay in registers, four consecutive ones a thread and turn, all of them requested at once; what a sequence has
+// beyond them is read again in every pass.
+template <int kTurns>
 __global__ __launch_bounds__(kThreads) void evict_choose(EvictArgs a, KvView kv) {
-    __shared__ uint32_t counts[2048], sums[2][kWaves];
+    // of each digit, four times over, a quarter of the lanes each: lanes that meet on one word wait for each other (30000 weights of which a tenth are zero:
+    // 39 us with one count)
+    __shared__ uint4 counts[2048];
+    __shared__ uint32_t sums[2][kWaves];
     __shared__ uint32_t found[2];                          // the digit, and how many of the tokens that have it are still to be taken
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / kv.kv_heads;
-    const int len = kv.length(kv.kv_len[b]);
+    const uint32_t len = kv.length(kv.kv_len[b]);
     const float* w = a.weights + (int64_t)blockIdx.x * a.stride;
     float* w_out = a.weights_out + (int64_t)blockIdx.x * a.stride_out;
     int32_t* kept = a.kept + (int64_t)blockIdx.x * a.keep;
-    const int late = len <= a.keep ? 0 : len - a.recent;   // the first of the tokens that stay for being the last ones
+    const uint32_t keep = a.keep, recent = a.recent;
+    const uint32_t late = len <= keep ? 0 : len - recent;  // the first of the tokens that stay for being the last ones
+    const bool some = late > 0 && keep > recent;
+    struct Four { uint32_t rank[kEach]; };
+    auto fetch = [&](uint32_t turn) {
+        const uint32_t p = turn * kTurn + threadIdx.x * kEach;
+        float x[kEach] = {};
+        if (len >= kEach) {                                // one load without a condition, so that those of all turns go out together; behind the
+            const uint32_t at = min(p, len - kEach);       // last token whatever stands in the last four
+            __builtin_memcpy(x, w + at, sizeof x);
+            if (p - at & 1) x[0] = x[1], x[1] = x[2], x[2] = x[3];
+            if (p - at & 2) x[0] = x[2], x[1] = x[3];
+        } else if (p == 0) {
+#pragma unroll
+            for (int e = 0; e < kEach - 1; ++e) if ((uint32_t)e < len) x[e] = w[e];
+        }
+        Four f;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) f.rank[e] = rank_of(x[e]);
+        return f;
+    };
+    Four held[kTurns];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) held[t] = fetch(t);
+    const uint32_t turns = (len + kTurn - 1) / kTurn;
+    // `go` for each turn in front of `end`, with its number and its tokens
+    auto each_turn = [&](uint32_t end, auto go) {
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t)
+            if ((uint32_t)t < end) go((uint32_t)t, held[t]);
+        for (uint32_t t = kTurns; t < end; ++t) go(t, fetch(t));
+    };
     uint32_t least = 0, take = 0;                          // the rank of the last one of the others that stays, and how many of those that have it
-    if (late > 0 && a.keep > a.recent) {
+    if (some) {
         uint32_t prefix = 0, mask = 0;
-        take = a.keep - a.recent;
+        take = keep - recent;
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            for (int i = threadIdx.x; i < 2048; i += kThreads) counts[i] = 0;
+            for (int i = threadIdx.x; i < 2048; i += kThreads) counts[i] = uint4{0, 0, 0, 0};
             __syncthreads();
-            for (uint32_t i = threadIdx.x; i < (uint32_t)late; i += kThreads) {
-                const uint32_t u = rank_of(w[i]);
-                if ((u & mask) == prefix) atomicAdd(&counts[(u >> shift) & ((1u << bits) - 1)], 1u);
-            }
+            each_turn((late + kTurn - 1) / kTurn, [&](uint32_t t, const Four& f) {
+                const uint32_t first = t * kTurn + threadIdx.x * kEach;
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const uint32_t digit = (f.rank[e] >> shift) & ((1u << bits) - 1);
+                    const bool counted = (f.rank[e] & mask) == prefix && first + e < late;
+                    if (pass > 0) {                        // few, or many that are alike: lanes that all have one digit count it together
+                        const uint64_t who = __builtin_amdgcn_ballot_w64(counted);
+                        if (!who) continue;
+                        const uint32_t one = __builtin_amdgcn_readlane(digit, __builtin_ctzll(who));
+                        if (__builtin_amdgcn_ballot_w64(counted && digit == one) == who) {
+                            if (lane == __builtin_ctzll(who)) atomicAdd(&counts[one].x, (uint32_t)__builtin_popcountll(who));
+                            continue;
+                        }
+                    }
+                    if (counted) atomicAdd(&counts[digit].x + (lane & 3), 1u);
+                }
+            });
             __syncthreads();
             // from the largest digit down: two a thread, counts of those above them
             const int d = 2047 - 2 * threadIdx.x;
-            const uint32_t own = counts[d] + counts[d - 1];
+            auto count_of = [&](int digit) { const uint4 c = counts[digit]; return (c.x + c.y) + (c.z + c.w); };
+            const uint32_t high = count_of(d), own = high + count_of(d - 1);
             uint32_t all, above = wave_before(own, &all);
             if (lane == 0) sums[0][wave] = all;
             __syncthreads();
             for (int i = 0; i < wave; ++i) above += sums[0][i];
-            if (above < take && above + counts[d] >= take) found[0] = d, found[1] = take - above;
-            else if (above + counts[d] < take && above + own >= take) found[0] = d - 1, found[1] = take - above - counts[d];
+            if (above < take && above + high >= take) found[0] = d, found[1] = take - above;
+            else if (above + high < take && above + own >= take) found[0] = d - 1, found[1] = take - above - high;
             __syncthreads();
             prefix |= found[0] << shift;
             mask |= ((1u << bits) - 1) << shift;
             take = found[1];
+            least = prefix;
+            const bool all_of_it = take == count_of(found[0]);
             __syncthreads();
+            if (all_of_it && prefix) {                     // all that have the digit stay, and none needs to be told from another
+                least = prefix - 1, take = 0;
+                break;
+            }
         }
-        least = prefix;
     }
-    // Positions in order, kEach a thread and turn: above `least`, equal to it (as far as `take` goes), or late.  What has been counted in front of
-    // this turn is the same in all threads.
+    // Positions in order: those above `least`, equal to it (as far as `take` goes), or late.  What has been counted in front of a turn is the same in all
+    // threads.  A turn's tokens go to places in front of the next one's, and are all read in front of its barrier: the weights may stay where they are.
     uint32_t equal = 0, number = 0;
-    const uint32_t end = len, last = late;
-    const bool some = late > 0 && a.keep > a.recent;
-    for (uint32_t i0 = 0; i0 < end; i0 += kThreads * kEach) {
-        const uint32_t first = i0 + threadIdx.x * kEach;
-        float x[kEach];
-        uint32_t more = 0, same = 0;                       // bits
+    each_turn(turns, [&](uint32_t t, const Four& f) {
+        const uint32_t first = t * kTurn + threadIdx.x * kEach;
+        uint32_t more = 0, same = 0, before_more = 0, before_same = 0, all_more = 0, all_same = 0;      // more, same: bits
+        const bool inside = (t + 1) * kTurn <= late;       // no token of the turn stays for being late
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
-            const uint32_t p = first + e;
-            x[e] = p < end ? w[p] : 0.0f;
-            const uint32_t u = rank_of(x[e]);
-            if (p < end && (p >= last || (some && u > least))) more |= 1u << e;
-            else if (p < end && some && u == least) same |= 1u << e;
+            const uint32_t p = first + e, u = f.rank[e];
+            const bool is_more = inside ? some && u > least : p < len && (p >= late || (some && u > least));
+            const uint64_t m = __builtin_amdgcn_ballot_w64(is_more);
+            before_more = lanes_before(m, before_more);
+            all_more += __builtin_popcountll(m);
+            more |= (uint32_t)is_more << e;
+            if (take == 0) continue;
+            const bool is_same = u == least && p < late;
+            const uint64_t q = __builtin_amdgcn_ballot_w64(is_same);
+            before_same = lanes_before(q, before_same);
+            all_same += __builtin_popcountll(q);
+            same |= (uint32_t)is_same << e;
         }
-        uint32_t all, before = wave_before(__popc(more) | (uint32_t)__popc(same) << 16, &all);
-        if (lane == 0) sums[0][wave] = all;
-        __syncthreads();                                   // all of this turn has been read: what follows may write where it was
-        uint32_t total = 0;
+        if (lane == 0) sums[t & 1][wave] = all_more | all_same << 16;
+        __syncthreads();
+        const uint32_t each = sums[t & 1][lane & (kWaves - 1)];
+        uint32_t total = 0, front = 0;
+#pragma unroll
         for (int i = 0; i < kWaves; ++i) {
-            if (i == wave) before += total;
-            total += sums[0][i];
+            if (i == wave) front = total;
+            total += __builtin_amdgcn_readlane(each, i);
         }
-        uint32_t eq = equal + (before >> 16), to = number + (before & 0xFFFFu) + min(eq, take);
+        uint32_t eq = equal + (front >> 16) + before_same, to = number + (front & 0xFFFFu) + before_more + min(eq, take);
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const bool tie = same >> e & 1 && eq < take;
             eq += same >> e & 1;
             if ((more >> e & 1) || tie) {
                 kept[to] = (int32_t)(first + e);
-                w_out[to] = x[e];
+                w_out[to] = weight_of(f.rank[e]);
                 ++to;
             }
         }
         equal += total >> 16;
         number += total & 0xFFFFu;
-        __syncthreads();
-    }
+    });
 }
 
 __global__ __launch_bounds__(256) void evict_move(EvictArgs a, KvView kv, int blocks_out, int64_t tasks) {
@@ -177,7 +244,11 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, KvView kv, int bl
 hipError_t launch_kv_evict(const KvView& kv, const float* weights, int64_t stride, int keep, int recent, const int32_t* table_out, int64_t table_out_stride,
                            float* weights_out, int64_t stride_out, int32_t* len_out, int32_t* kept, hipStream_t stream) {
     const EvictArgs a{weights, weights_out, table_out, len_out, kept, stride, stride_out, table_out_stride, keep, recent};
-    evict_choose<<<(unsigned)((int64_t)kv.B * kv.kv_heads), kThreads, 0, stream>>>(a, kv);
+    const unsigned pairs = (unsigned)((int64_t)kv.B * kv.kv_heads);
+    const int64_t turns = ceil_div((int64_t)kv.max_blocks * kKvBlock, kTurn);
+    if (turns <= 1) evict_choose<1><<<pairs, kThreads, 0, stream>>>(a, kv);
+    else if (turns <= 4) evict_choose<4><<<pairs, kThreads, 0, stream>>>(a, kv);
+    else evict_choose<10><<<pairs, kThreads, 0, stream>>>(a, kv);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t most = (int64_t)kv.max_blocks * kKvBlock;
