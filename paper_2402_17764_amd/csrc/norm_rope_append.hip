@@ -8,7 +8,7 @@
 namespace bitnet {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kGains = 256;
 
 struct NormShape {
     const float *q_gain, *k_gain;      // [D] or NULL
@@ -17,7 +17,16 @@ struct NormShape {
     int norm;                          // 0: heads are turned as they are
 };
 
-// 1 / sqrt(mean + eps) in 32 bits: the instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is.
+// 1 / sqrt(mean + eps).  A sum of squares that 32 bits hold with room on both sides takes the 32-bit instruction (within 2^-23); the others are summed up
+// again in 64 bits, with the 64-bit instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is.
+__device__ inline bool in_range(float sum) { return sum > 1e-30f && sum < 1e37f; }
+__device__ inline float head_scale(float sum, float inv_d, float eps) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_d, eps));
+#else
+    return 0.0f;
+#endif
+}
 __device__ inline float head_scale(double sum, double inv_d, float eps) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const double a = __builtin_fma(sum, inv_d, (double)eps);
@@ -29,14 +38,37 @@ __device__ inline float head_scale(double sum, double inv_d, float eps) {
 #endif
 }
 
-template <bool kBf16>
-__device__ inline double squares_of(const Eight<kBf16>& v, int count) {
+template <bool kBf16, typename Sum>
+__device__ inline Sum squares_of(const Eight<kBf16>& v, int count) {
     float x[8];
     floats_of<kBf16>(x, v);
-    double s = 0.0;
+    Sum s = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s = e < count ? __builtin_fma((double)x[e], (double)x[e], s) : s;
+    for (int e = 0; e < 8; ++e) {
+        const Sum y = e < count ? (Sum)x[e] : (Sum)0;
+        if constexpr (sizeof(Sum) == 4) s = __builtin_fmaf(y, y, s);
+        else s = __builtin_fma(y, y, s);
+    }
     return s;
+}
+// the sum over kLanes neighbouring lanes
+template <int kLanes>
+__device__ inline float lanes_sum(float v) {
+    v += dpp_f32<0xB1>(v);
+    v += dpp_f32<0x4E>(v);
+    v += dpp_f32<0x141>(v);
+    if (kLanes >= 16) v += dpp_f32<0x140>(v);
+    if (kLanes >= 32) v += __shfl_xor(v, 16);
+    return v;
+}
+template <int kLanes>
+__device__ inline double lanes_sum(double v) {
+    v += dpp_f64<0xB1>(v);
+    v += dpp_f64<0x4E>(v);
+    v += dpp_f64<0x141>(v);
+    if (kLanes >= 16) v += dpp_f64<0x140>(v);
+    if (kLanes >= 32) v += __shfl_xor(v, 16);
+    return v;
 }
 
 // x[e] *= r gain[d + e], of the dims in front of `end`; gain NULL: ones
@@ -113,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_tokens(const void* 
     }
     const double at = (double)pos + (double)(w.shift ? w.shift[b] : 0);
     for (int i = threadIdx.x; i < s.rotary >> 1; i += kThreads) turns[i] = turn_of(at, inv_freq[i]);
-    if (w.norm && turned) squares[threadIdx.x] = squares_of<kBf16>(slot.own, D - d0);
+    if (w.norm && turned) squares[threadIdx.x] = squares_of<kBf16, double>(slot.own, D - d0);
     __syncthreads();
     if (!mine) return;
     float x[8], none[8];
@@ -165,6 +197,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
                                                                     RopeShape s, int per, uint16_t* __restrict__ q) {
     constexpr int kM = kLanes / 8, kTokens = kThreads / kLanes, kPitch = 256 + 8;      // tokens of a workgroup at a time
     __shared__ uint4 tile4[kKvBlock * kPitch / 8];
+    __shared__ __attribute__((aligned(16))) float gain_of[2 * kGains];                 // of queries, of keys: ones where there is none
     uint16_t* tile = reinterpret_cast<uint16_t*>(tile4);
     const int D = kv.D, Dp = kv_padded_dim(D), units = s.heads + 2 * kv.kv_heads, keys = s.heads + kv.kv_heads;
     const int b = sequence_of_tile(kv.q_start, kv.B, blockIdx.x, 1, kKvBlock, 2);
@@ -178,8 +211,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
     const int row0 = nt.first + blk * kKvBlock - nt.pos0;      // of token 0 of the block
     const int u0 = blockIdx.y * per, u1 = min(u0 + per, units);
     const int page_index = blk >= 0 ? blk / kv.page_blocks : 0, page = blk >= 0 ? kv.table[b * kv.table_stride + page_index] : -1;
-    const double shift = w.shift ? (double)w.shift[b] : 0.0, inv_d = 1.0 / D;
-
+    const double shift = w.shift ? (double)w.shift[b] : 0.0;
+    const float inv_d = 1.0f / D;
     const int half = s.rotary >> 1, half8 = (half + 7) >> 3, slots = slots_of<kTurned>(D, s);
     const int j = threadIdx.x & (kLanes - 1);
     const int d0 = kTurned == Turned::Split && j >= half8 ? s.rotary + 8 * (j - half8) : 8 * j;
@@ -197,9 +230,6 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
                 turn[m][e] = d0 + e < s.rotary ? turn_of((double)(blk * kKvBlock + tok[m]) + shift, inv_freq[pair_of(d0 + e, s)]) : Turn{1.0f, 0.0f};
             }
     }
-    float g[8], partner[8];
-    auto gains = [&](bool query) { gains_for<kTurned>(g, partner, w.norm && j < slots ? (query ? w.q_gain : w.k_gain) : nullptr, d0, D, s); };
-    if (u0 < keys) gains(u0 < s.heads);
     Slot<kBf16, kTurned> slot[kM], next[kM];
     auto request = [&](Slot<kBf16, kTurned> (&x)[kM], int u) {
 #pragma unroll
@@ -207,13 +237,18 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
             if (tok[m] >= 0) x[m].load(qkv, ((int64_t)(row0 + tok[m]) * units + u) * D, (int64_t)(units - u) * D, d0, D, u < keys, s);
     };
     request(next, u0);
+    for (int i = threadIdx.x; i < 2 * kGains; i += kThreads) {
+        const float* gain = !w.norm ? nullptr : i < kGains ? w.q_gain : w.k_gain;
+        const int d = i & (kGains - 1);
+        gain_of[i] = gain && d < D ? gain[d] : 1.0f;
+    }
+    __syncthreads();
 #pragma unroll 1
     for (int u = u0; u < u1; ++u) {
 #pragma unroll
         for (int m = 0; m < kM; ++m) slot[m] = next[m];
         if (u + 1 < u1) request(next, u + 1);
         const bool query = u < s.heads, key = !query && u < keys;
-        if (u == s.heads && u > u0) gains(false);
         int block = -1;
         if (!query) block = kv.block_on(page, blk - page_index * kv.page_blocks, key ? u - s.heads : u - keys);
         if (!query && block < 0) continue;                     // the same for the whole workgroup
@@ -222,17 +257,20 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
         for (int m = 0; m < kM; ++m) {
             float r = 1.0f;
             if (w.norm && (query || key)) {                    // all lanes: the sum goes over neighbours
-                double sum = 0.0;
-                if (tok[m] >= 0) {
-                    sum = squares_of<kBf16>(slot[m].own, D - d0);
-                    if (both) sum += squares_of<kBf16>(slot[m].low, 8);
-                }
-                sum += dpp_f64<0xB1>(sum);
-                sum += dpp_f64<0x4E>(sum);
-                sum += dpp_f64<0x141>(sum);
-                if (kLanes >= 16) sum += dpp_f64<0x140>(sum);
-                if (kLanes >= 32) sum += __shfl_xor(sum, 16);
+                auto squares = [&](auto zero) {
+                    auto sum = zero;
+                    if (tok[m] >= 0) {
+                        sum = squares_of<kBf16, decltype(zero)>(slot[m].own, D - d0);
+                        if (both) sum += squares_of<kBf16, decltype(zero)>(slot[m].low, 8);
+                    }
+                    return lanes_sum<kLanes>(sum);
+                };
+                const float sum = squares(0.0f);
                 r = head_scale(sum, inv_d, w.eps);
+                if (__builtin_amdgcn_ballot_w64(tok[m] >= 0 && !in_range(sum))) {
+                    const float far = head_scale(squares(0.0), 1.0 / D, w.eps);
+                    if (!in_range(sum)) r = far;
+                }
             }
             if (tok[m] < 0) continue;
             const int64_t out = ((int64_t)(row0 + tok[m]) * s.heads + u) * D;
@@ -243,6 +281,13 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
             };
             float x[8], y[8];
             if (query || key) {
+                float g[8], partner[8];
+                const float* gain = gain_of + (query ? 0 : kGains);
+                __builtin_memcpy(g, __builtin_assume_aligned(gain + d0, 16), sizeof g);
+                if (kTurned == Turned::Split) __builtin_memcpy(partner, __builtin_assume_aligned(gain + (both ? d0 + half : d0), 16), sizeof partner);
+                if (kTurned == Turned::Any)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) partner[e] = gain[d0 + e < half ? d0 + e + half : max(d0 + e - half, 0)];
                 norm_and_turn(x, y, slot[m], d0, r, g, partner, turn[m], s);
             } else {
                 floats_of<kBf16>(x, slot[m].own);

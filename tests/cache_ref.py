@@ -6,8 +6,10 @@ from attention_ref import F32_HALF_STEP, rope
 
 
 def norm_rope(x, pos, freq, pairs, gain, eps, norm):
-    """x [n, heads, D] fp64 -> (normed and turned, bound of the fp32 steps).  A head's factor is rounded to fp32 (half a step, behind an instruction
-    and one Newton step in 64 bits, which leave less than that), its two products a half step each; they go through the turn with both of a pair."""
+    """x [n, heads, D] fp64 -> (normed and turned, bound of the fp32 steps).  A head's sum of squares is one of positive terms in fp32: up to 16 steps of a
+    lane and 5 between lanes, a half step of the sum each, so 21, of which the root takes half; the mean's product and the sum with eps one each, of
+    which the root takes half; the root's instruction two: 13.5 half steps on the factor.  Its two products have one each, and go
+    through the turn with both of a pair."""
     if not norm:
         return rope(x, pos, freq, pairs)
     s = (x * x).mean(axis=-1, keepdims=True)
@@ -17,7 +19,7 @@ def norm_rope(x, pos, freq, pairs, gain, eps, norm):
     size = np.abs(y)
     a = (slice(0, r, 2), slice(1, r, 2)) if pairs else (slice(0, half), slice(half, r))
     size[..., a[0]] = size[..., a[1]] = size[..., a[0]] + size[..., a[1]]
-    return z, off + 4 * F32_HALF_STEP * size
+    return z, off + 15.5 * F32_HALF_STEP * size
 
 
 def weights(q, k, seen, scale):
