@@ -593,10 +593,10 @@ bitnet_status bitnet_norm_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype
  *                  page that the prefix fills in part may be another one in each row.  A sequence of fewer tokens sees those it has.
  *   prefixes       at least 1, prefixes*heads < 2^22 (BITNET_ERR_SHAPE otherwise); runs may be empty
  *   workspace      device memory, 16-byte aligned, of the bitnet_attention_shared_workspace() bytes or more (BITNET_ERR_WORKSPACE otherwise; it is needed here)
- *   Weights enter their product as in bitnet_attention_prefill for the shared tokens, as in bitnet_attention_decode for a sequence's own.
+ *   Weights enter their product as in bitnet_attention_prefill (of a BF16 result's own tokens as in bitnet_attention_decode, for groups of many rows).
  *   kv->q_start is not read.
  */
-bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, size_t* bytes);
+bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, bitnet_dtype o_dtype, size_t* bytes);
 bitnet_status bitnet_attention_decode_shared(const void* q, const bitnet_kv* kv, const int32_t* prefix_start, const int32_t* prefix_len, int64_t prefixes,
                                              int64_t heads, float scale, void* o, bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream);
 

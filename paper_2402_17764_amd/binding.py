@@ -108,7 +108,7 @@ def load():
     lib.bitnet_attention_decode.argtypes = [vp, kvp, i64, ctypes.c_float, vp, ci, vp, sz, vp]
     lib.bitnet_attention_prefill.argtypes = [vp, kvp, i64, i64, ctypes.c_float, vp, ci, vp, sz, vp]
     lib.bitnet_norm_rope_kv_append.argtypes = [vp, ci, ci, vp, vp, ctypes.c_float, vp, i64, ci, vp, kvp, i64, i64, vp, vp]
-    lib.bitnet_attention_shared_workspace.argtypes = [kvp, i64, i64, szp]
+    lib.bitnet_attention_shared_workspace.argtypes = [kvp, i64, i64, ci, szp]
     lib.bitnet_attention_decode_shared.argtypes = [vp, kvp, vp, vp, i64, i64, ctypes.c_float, vp, ci, vp, sz, vp]
     lib.bitnet_attention_weights_workspace.argtypes = [kvp, i64, i64, ci, ci, szp]
     lib.bitnet_attention_decode_weights.argtypes = [vp, kvp, i64, ctypes.c_float, vp, ci, vp, i64, vp, sz, vp]
@@ -404,12 +404,12 @@ def attention_workspace(T, heads, head_dim, k_cache, page_table, prefill=False):
     return int(out.value)
 
 
-def attention_shared_workspace(prefixes, heads, head_dim, k_cache, page_table):
+def attention_shared_workspace(prefixes, heads, head_dim, k_cache, page_table, y_dtype=BF16):
     """Bytes of scratch that attention_decode_shared needs."""
     lib = load()
     out = ctypes.c_size_t(0)
-    _check(lib.bitnet_attention_shared_workspace(ctypes.byref(_kv_for_query(head_dim, k_cache, page_table)), prefixes, heads, ctypes.byref(out)),
-           "bitnet_attention_shared_workspace")
+    _check(lib.bitnet_attention_shared_workspace(ctypes.byref(_kv_for_query(head_dim, k_cache, page_table)), prefixes, heads, y_dtype,
+                                                 ctypes.byref(out)), "bitnet_attention_shared_workspace")
     return int(out.value)
 
 

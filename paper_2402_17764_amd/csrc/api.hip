@@ -677,13 +677,14 @@ bitnet_status bitnet_norm_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype
                                                     view, T, (int)heads, q, static_cast<hipStream_t>(stream)));
 }
 
-bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, size_t* bytes) {
+bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, bitnet_dtype o_dtype, size_t* bytes) {
     if (!bytes) return BITNET_ERR_NULL;
     bitnet::KvView view;
     const bitnet_status st = kv_view(kv, kv ? kv->sequences : 1, heads, &view);
     if (st != BITNET_OK) return st;
     if (prefixes <= 0 || prefixes > kMaxSequenceHeads / heads) return BITNET_ERR_SHAPE;
-    *bytes = bitnet::attention_shared_workspace_bytes(view, (int)prefixes, (int)heads);
+    if (o_dtype != BITNET_F32 && o_dtype != BITNET_BF16) return BITNET_ERR_DTYPE;
+    *bytes = bitnet::attention_shared_workspace_bytes(view, (int)prefixes, (int)heads, o_dtype == BITNET_F32);
     return BITNET_OK;
 }
 
@@ -695,7 +696,7 @@ bitnet_status bitnet_attention_decode_shared(const void* q, const bitnet_kv* kv,
     if (st != BITNET_OK) return st;
     if (prefixes <= 0 || prefixes > kMaxSequenceHeads / heads) return BITNET_ERR_SHAPE;
     if (!aligned(prefix_start, 4) || !aligned(prefix_len, 4)) return BITNET_ERR_ALIGN;
-    if (workspace_bytes < bitnet::attention_shared_workspace_bytes(view, (int)prefixes, (int)heads)) return BITNET_ERR_WORKSPACE;
+    if (workspace_bytes < bitnet::attention_shared_workspace_bytes(view, (int)prefixes, (int)heads, o_dtype == BITNET_F32)) return BITNET_ERR_WORKSPACE;
     return from_hip(bitnet::launch_attention_shared(q, view, prefix_start, prefix_len, (int)prefixes, (int)heads, scale, o, o_dtype == BITNET_F32, workspace,
                                                     static_cast<hipStream_t>(stream)));
 }

@@ -211,6 +211,10 @@ __device__ inline int token_of(int row, int group) { return (int)((unsigned)row 
 __device__ inline int tile_sees(const NewTokens& nt, int row_last, int group) { return nt.pos0 + token_of(row_last, group) + 1; }
 __device__ inline int stages_of(int seen) { return seen > 0 ? (seen + kStageTokens - 1) / kStageTokens : 0; }
 
+// `unit` tokens at a time, those that hold some of a sequence's own, behind `shared` ones: the first, and how many
+__device__ inline int own_first(int shared, int unit) { return shared / unit; }
+__device__ inline int own_units(int len, int shared, int unit) { return shared >= len ? 0 : (len + unit - 1) / unit - own_first(shared, unit); }
+
 __device__ inline int blocks_of(const KvView& kv, int b) { return (kv.length(kv.kv_len[b]) + kKvBlock - 1) / kKvBlock; }
 
 // The kernel for a head's size: `go` is called with the sizes that it is built for, kC chunks of 32 dims and kV tiles of 16, as types

@@ -22,8 +22,8 @@ struct DecodeArgs {
     int column_tiles;                  // of 16 query heads, per key-value head
 };
 
-// What a launch does: all of a row's attention; the part of it behind what its sequence shares with others (the splits of a row stand behind
-// `first` of the shared part's, `pitch` in all); or all of it, with the row's scores and softmax state for the weights of the tokens.
+// What a launch does: all of a row's attention; the part of it behind what its sequence shares with others (a row's splits stand behind `first` others,
+// `pitch` in all); or all of it, leaving the row's scores and softmax state too, for the weights of the tokens.
 enum class Single { All, Own, Scored };
 struct SingleMore {
     Prefixes prefixes;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
     const int len = kv.length(kv.kv_len[b]), blocks = (len + kKvBlock - 1) / kKvBlock;
     int shared = 0;                                        // tokens that this launch leaves out, the first ones
     if constexpr (kDo == Single::Own) shared = shared_tokens(kv, more.prefixes, b, len);
-    const int begin = kDo == Single::Own ? own_first(shared) : 0, units = kDo == Single::Own ? own_blocks(len, shared) : blocks;
+    const int begin = kDo == Single::Own ? own_first(shared, kKvBlock) : 0, units = kDo == Single::Own ? own_units(len, shared, kKvBlock) : blocks;
     const int run = parts.run(units), blk0 = begin + (int)blockIdx.y * run, blk1 = min(blk0 + run, blocks);
     if (kDo == Single::Own ? blk0 - begin >= units : blk0 >= blocks && blockIdx.y > 0) return;
 

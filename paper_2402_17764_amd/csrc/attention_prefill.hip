@@ -48,7 +48,7 @@ static hipError_t launch_runs(const void* q, const KvView& kv, int64_t T, int he
         if (keep.state && !f32) keep.totals = reinterpret_cast<float*>(static_cast<char*>(workspace) + bytes);
     }
     const hipError_t e = for_head_size(kv.D, [&](auto c, auto v, auto exact) {
-        if (keep.state) return launch_prefill_kept<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, RowsMore{keep, {}, 0}, stream);
+        if (keep.state) return launch_prefill_kept<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, RowsMore{keep, {}}, stream);
         return launch_prefill<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, stream);
     });
     if (e != hipSuccess || parts.splits < 2) return e;

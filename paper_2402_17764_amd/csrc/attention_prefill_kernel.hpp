@@ -25,13 +25,22 @@ struct PrefillArgs {
 };
 
 // Whose rows a launch takes: runs of new tokens, causal; the same, leaving each row's softmax state (of weights as they are, not as they are rounded)
-// for the weights of the keys; or the single new tokens of sequences that share their first tokens, over those alone, as the first
-// parts of rows that have `pitch` of them.
-enum class Rows { Causal, Kept, Shared };
+// for the weights of the keys; or the single new tokens of sequences that share their first tokens, as parts of rows: over those of a group alone, its
+// sequences in place of new tokens, or over what each sequence has behind them as well.
+enum class Rows { Causal, Kept, Prefix, Shared };
+constexpr bool of_groups(Rows r) { return r == Rows::Prefix || r == Rows::Shared; }
+struct SharedLaunch {
+    Prefixes prefixes;
+    uint32_t near_blocks, far_blocks;  // workgroups of a key-value head over what is shared (tiles of rows times splits), and over what is not
+    uint32_t far_ratio;                // far_blocks 2^32 / (near_blocks + far_blocks), rounded up
+    int near, far;                     // splits of a row over either; their parts stand behind one another
+    int least_near, least_far;         // units of tokens that a split has at least
+    int far_tiles;                     // of a sequence's rows, per key-value head
+    int far_unit;                      // tokens: a stage's, or a block's if another launch takes what is not shared
+};
 struct RowsMore {
     KeptRows keep;                     // Kept
-    Prefixes prefixes;                 // Shared
-    int pitch;
+    SharedLaunch shared;
 };
 
 // The shapes of a workgroup: four waves of one or two times 16 rows each (heads of more than 128 dims: four or eight waves of 16, as a wave's
@@ -72,32 +81,76 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         piece_from[j] = 16 * (p < kKeyLoads ? min(key >> 5, (Dp >> 3) - 1) * 32 + (key & 31) : value / (16 * kV) * Dp + min(value % (16 * kV), Dp - 1));
     }
 
-    // Heads side by side: with a multiple of eight of them a head's tiles meet on one XCD, whose L2 then holds its keys and values once.
-    const int h = blockIdx.x % kv.kv_heads;
-    const int64_t x = a.tiles - 1 - (int)(blockIdx.x / kv.kv_heads);       // late tiles, which see most, first
-    // of shared rows: a group in a sequence's place, its sequences in that of new tokens
-    const int32_t* start;
-    int b;
-    if constexpr (kOf == Rows::Shared) start = more.prefixes.start, b = sequence_of_tile(start, more.prefixes.groups, x, a.group, kRows, 1);
-    else start = kv.q_start, b = sequence_of_tile(start, kv.B, x, a.group, kRows, 1);
-    const auto nt = [&] {
-        if constexpr (kOf == Rows::Shared) return SharedRows(kv, more.prefixes, b);
-        else return NewTokens(kv, b, a.T);
-    }();
-    // tokens times heads are below 2^28, so rows have 32 bits: 64-bit quotients are a hundred instructions each in front of the first load
-    const int64_t tile = x - first_tile(start[b], b, a.group, kRows, 1);
-    const int rows = nt.n * a.group;                                       // of the sequence, for this head
-    if (tile < 0 || tile * kRows >= rows) return;
-    const int row0 = (int)tile * kRows;
-    const int row_last = min(row0 + kRows, rows) - 1;
-    int seen;                                                              // keys that the tile's last token sees, or that all share
-    if constexpr (kOf == Rows::Shared) seen = nt.len;
-    else seen = tile_sees(nt, row_last, a.group);
-    const int blocks = seen > 0 ? (seen + kKvBlock - 1) / kKvBlock : 0, all_stages = stages_of(seen);
-    // this workgroup's stages
-    const int run = parts.run(all_stages), stage0 = blockIdx.y * run * kPerUnit;
-    const int stages = min(stage0 + run * kPerUnit, (blocks + kStageBlocks - 1) / kStageBlocks);
-    if (blockIdx.y > 0 && stage0 >= stages) return;
+    int h, row0, rows, row_last, seen; [[maybe_unused]] int front = 0;       // front, seen: the first key that the tile's rows see, and the end of the last row's
+    int blocks, all_stages, run, split, stage0, stages;
+    const int32_t* table = kv.table;
+    int first_row, pos0;                                                   // the rows' first token among all, and its position
+    if constexpr (of_groups(kOf)) {
+        const SharedLaunch& l = more.shared;
+        // The two kinds of workgroups mixed evenly: those over shared tokens are bound by their matrix instructions, the others by memory.
+        // Heads side by side, so that with a multiple of eight of them a head's tiles meet on one XCD.
+        const uint32_t x = blockIdx.x / (uint32_t)kv.kv_heads, far_before = kOf == Rows::Shared ? (uint32_t)((uint64_t)x * l.far_ratio >> 32) : 0;
+        const bool far = kOf == Rows::Shared && (uint32_t)((uint64_t)(x + 1) * l.far_ratio >> 32) > far_before;
+        const uint32_t i = far ? far_before : x - far_before;
+        h = (int)(blockIdx.x - x * (uint32_t)kv.kv_heads);
+        int first_unit = 0;
+        if (far) {
+            const uint32_t each = i / l.far_tiles;
+            const int tile = (int)(i - each * l.far_tiles), b = (int)(each % kv.B);
+            split = (int)(each / kv.B);
+            rows = a.group;
+            row0 = tile * kRows;
+            seen = kv.length(kv.kv_len[b]);
+            front = shared_tokens(kv, l.prefixes, b, seen);
+            first_row = b;
+            first_unit = own_first(front, kStageTokens);
+            all_stages = own_units(seen, front, kStageTokens);
+            run = max((all_stages + l.far - 1) / l.far, l.least_far);
+        } else {
+            split = (int)(i / a.tiles);
+            const int64_t t = i - (uint32_t)split * a.tiles;
+            const int b = sequence_of_tile(l.prefixes.start, l.prefixes.groups, t, a.group, kRows, 1);
+            const SharedRows r(kv, l.prefixes, b);
+            const int64_t tile = t - first_tile(l.prefixes.start[b], b, a.group, kRows, 1);
+            rows = r.n * a.group;
+            if (tile < 0 || tile * kRows >= rows) return;
+            row0 = (int)tile * kRows;
+            seen = r.len;
+            first_row = r.first;
+            all_stages = stages_of(seen);
+            run = max((all_stages + l.near - 1) / l.near, l.least_near);
+        }
+        if (split * run >= all_stages) return;
+        row_last = min(row0 + kRows, rows) - 1;
+        blocks = (seen + kKvBlock - 1) / kKvBlock;
+        stage0 = (first_unit + split * run) * kPerUnit;
+        stages = min(stage0 + run * kPerUnit, (blocks + kStageBlocks - 1) / kStageBlocks);
+        table += first_row * kv.table_stride;
+        split += far ? l.near : 0;
+        pos0 = 0;
+    } else {
+        // Heads side by side: with a multiple of eight of them a head's tiles meet on one XCD, whose L2 then holds its keys and values once.
+        h = blockIdx.x % kv.kv_heads;
+        const int64_t x = a.tiles - 1 - (int)(blockIdx.x / kv.kv_heads);       // late tiles, which see most, first
+        const int b = sequence_of_tile(kv.q_start, kv.B, x, a.group, kRows, 1);
+        const NewTokens nt(kv, b, a.T);
+        // tokens times heads are below 2^28, so rows have 32 bits: 64-bit quotients are a hundred instructions each in front of the first load
+        const int64_t tile = x - first_tile(kv.q_start[b], b, a.group, kRows, 1);
+        rows = nt.n * a.group;                                                 // of the sequence, for this head
+        if (tile < 0 || tile * kRows >= rows) return;
+        row0 = (int)tile * kRows;
+        row_last = min(row0 + kRows, rows) - 1;
+        seen = tile_sees(nt, row_last, a.group);                               // keys that the tile's last token sees
+        blocks = seen > 0 ? (seen + kKvBlock - 1) / kKvBlock : 0, all_stages = stages_of(seen);
+        // this workgroup's stages
+        run = parts.run(all_stages), stage0 = blockIdx.y * run * kPerUnit;
+        stages = min(stage0 + run * kPerUnit, (blocks + kStageBlocks - 1) / kStageBlocks);
+        if (blockIdx.y > 0 && stage0 >= stages) return;
+        split = blockIdx.y;
+        table += b * kv.table_stride;
+        first_row = nt.first;
+        pos0 = nt.pos0;
+    }
 
     v8bf qf[kNT][kC];
     int pos[kNT];                                                          // of the lane's queries; -1: none
@@ -106,18 +159,17 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         const int R = wave_row + 16 * n + r, tok = token_of(R, a.group), hh = R - tok * a.group;
-        out_row[n] = R < rows ? (nt.first + tok) * a.heads + h * a.group + hh : -1;
-        if constexpr (kOf == Rows::Shared) pos[n] = R < rows ? min(kv.length(kv.kv_len[nt.first + tok]), nt.len) - 1 : -1;
-        else pos[n] = R < rows ? nt.pos0 + tok : -1;
+        out_row[n] = R < rows ? (first_row + tok) * a.heads + h * a.group + hh : -1;
+        if constexpr (of_groups(kOf)) pos[n] = R < rows ? min(kv.length(kv.kv_len[first_row + tok]), seen) - 1 : -1;
+        else pos[n] = R < rows ? pos0 + tok : -1;
         load_query<kC, kExact>(qf[n], R < rows ? a.q + (int64_t)out_row[n] * D : nullptr, g, D);
     }
     int tile_pos, pos_last;                                                 // of the tile's first token, and of the wave's last
-    const int32_t* table = kv.table;
-    if constexpr (kOf == Rows::Shared) {                                    // the least of the tile, and the most
+    if constexpr (of_groups(kOf)) {                                         // the least of the tile, and the most
         const int tok0 = token_of(row0, a.group), toks = token_of(row_last, a.group) - tok0 + 1;
         int least = 0x7FFFFFFF, most = 0;
         for (int i = lane; i < toks; i += 64) {
-            const int n = min(kv.length(kv.kv_len[nt.first + tok0 + i]), nt.len);
+            const int n = min(kv.length(kv.kv_len[first_row + tok0 + i]), seen);
             least = min(least, n);
             most = max(most, n);
         }
@@ -128,11 +180,9 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         }
         tile_pos = __builtin_amdgcn_readfirstlane(least) - 1;
         pos_last = wave_row < rows ? __builtin_amdgcn_readfirstlane(most) - 1 : -1;
-        table += nt.first * kv.table_stride;
     } else {
-        tile_pos = nt.pos0 + token_of(row0, a.group);
-        pos_last = wave_row < rows ? nt.pos0 + token_of(min(wave_row + 16 * kNT, rows) - 1, a.group) : -1;
-        table += b * kv.table_stride;
+        tile_pos = pos0 + token_of(row0, a.group);
+        pos_last = wave_row < rows ? pos0 + token_of(min(wave_row + 16 * kNT, rows) - 1, a.group) : -1;
     }
     int numbers = -1;                                                      // of 64 blocks, one a lane
     auto fetch_numbers = [&](int blk0) {
@@ -231,7 +281,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 if (kMasked)
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (!known[u] || j0 + u * kKvBlock + 8 * g + j > pos[n]) sc[u][j >> 2][n][j & 3] = kMinusInf;
+                        if (!known[u] || j0 + u * kKvBlock + 8 * g + j > pos[n] || (kOf == Rows::Shared && j0 + u * kKvBlock + 8 * g + j < front)) sc[u][j >> 2][n][j & 3] = kMinusInf;
                 float top = sc[u][0][n][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[u][j >> 2][n][j & 3]);
@@ -304,6 +354,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
             uint4* place = reinterpret_cast<uint4*>(values + i * 16);
             v4u v = __builtin_bit_cast(v4u, *place);
             values_keep(v, some);
+            if (kOf == Rows::Shared && first < front) values_drop(v, front - first);
             unsigned bad = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) bad |= (unsigned)((v[e] & 0x7F80u) == 0x7F80u) | (unsigned)((v[e] & 0x7F800000u) == 0x7F800000u);
@@ -315,21 +366,23 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                     atomicMin(&bad_at[d], first + e);
                 }
             }
-            if (bad || some < 8) *place = __builtin_bit_cast(uint4, v);
+            if (bad || some < 8 || (kOf == Rows::Shared && first < front)) *place = __builtin_bit_cast(uint4, v);
         }
     };
     int s = stage0;
-    // Stages that all rows of the tile see, and all of whose pages exist; then the others.
-    for (; s < stages; ++s) {
+    auto whole_stage = [&](int s) {                                        // that all rows of the tile see, and all of whose pages exist
         const int j0 = s * kStageBlocks * kKvBlock, at = (s * kStageBlocks) & 63;
-        if (j0 + kStageBlocks * kKvBlock - 1 > tile_pos || __builtin_amdgcn_readlane(numbers, at) < 0 || __builtin_amdgcn_readlane(numbers, at + kStageBlocks - 1) < 0) break;
+        return (kOf != Rows::Shared || j0 >= front) && j0 + kStageBlocks * kKvBlock - 1 <= tile_pos && __builtin_amdgcn_readlane(numbers, at) >= 0 &&
+               __builtin_amdgcn_readlane(numbers, at + kStageBlocks - 1) >= 0;
+    };
+    auto plain_stage = [&](int s) {
         stage_there(s);
         const char* keys = lds + (s & 1) * kStage;
         const char* values = keys + kStageBlocks * kKeyPiece;
         const bool known[kU] = {};
-        take(std::false_type(), keys, values, j0, known);
-    }
-    for (; s < stages; ++s) {
+        if (kOf != Rows::Shared || wave_row < rows) take(std::false_type(), keys, values, s * kStageBlocks * kKvBlock, known);
+    };
+    auto masked_stage = [&](int s) {
         const int j0 = s * kStageBlocks * kKvBlock;
         bool known[kStageBlocks];
 #pragma unroll
@@ -339,8 +392,16 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         char* values = keys + kStageBlocks * kKeyPiece;
         clean(values, j0, known);
         __syncthreads();
-        if (j0 > pos_last) continue;                                       // nothing that this wave's rows see
+        if (j0 > pos_last) return;                                         // nothing that this wave's rows see
         take(std::true_type(), keys, values, j0, known);
+    };
+    if constexpr (kOf == Rows::Shared) {                                   // the first stage may begin with shared tokens
+        for (; s < stages; ++s)
+            if (whole_stage(s)) plain_stage(s);
+            else masked_stage(s);
+    } else {
+        for (; s < stages && whole_stage(s); ++s) plain_stage(s);
+        for (; s < stages; ++s) masked_stage(s);
     }
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
@@ -348,9 +409,8 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         [[maybe_unused]] float kept = total;
         if constexpr (kBoth) kept = groups_sum(whole_l[n]);
         if (out_row[n] < 0) continue;
-        int64_t place = (int64_t)out_row[n] * parts.splits + blockIdx.y;
-        if constexpr (kOf == Rows::Shared) place = (int64_t)out_row[n] * more.pitch + blockIdx.y;
-        const bool whole = kOf != Rows::Shared && run >= all_stages;
+        const int64_t place = (int64_t)out_row[n] * parts.splits + split;
+        const bool whole = !of_groups(kOf) && run >= all_stages;
         const float by = whole ? inv : 1.0f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
@@ -385,9 +445,12 @@ hipError_t launch_prefill_tiles(PrefillArgs a, const Parts& parts, const KvView&
         const hipError_t e = raise_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds, raised);
         if (e != hipSuccess) return e;
     }
-    if constexpr (kOf == Rows::Shared) a.tiles = (int)tiles_at_most(kv.B, more.prefixes.groups, a.group, 16 * kNT * kW, 1);
-    else a.tiles = (int)tiles_at_most(a.T, kv.B, a.group, 16 * kNT * kW, 1);
-    kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, kLds, stream>>>(a, parts, kv, more);
+    if constexpr (of_groups(kOf)) {
+        kernel<<<(more.shared.near_blocks + more.shared.far_blocks) * kv.kv_heads, 64 * kW, kLds, stream>>>(a, parts, kv, more);
+    } else {
+        a.tiles = (int)tiles_at_most(a.T, kv.B, a.group, 16 * kNT * kW, 1);
+        kernel<<<dim3((unsigned)((int64_t)a.tiles * kv.kv_heads), parts.splits), 64 * kW, kLds, stream>>>(a, parts, kv, more);
+    }
     return hipGetLastError();
 }
 template <int kC, int kV, bool kExact, bool kF32, Rows kOf, typename More>
@@ -409,8 +472,16 @@ hipError_t launch_prefill_kept(PrefillTile tile, const PrefillArgs& a, const Par
 }
 template <int kC, int kV, bool kExact>
 hipError_t launch_prefill_shared(PrefillTile tile, const PrefillArgs& a, const Parts& parts, const KvView& kv, bool f32, const RowsMore& more, hipStream_t stream) {
-    return f32 ? launch_prefill_form<kC, kV, kExact, true, Rows::Shared>(tile, a, parts, kv, more, stream)
-               : launch_prefill_form<kC, kV, kExact, false, Rows::Shared>(tile, a, parts, kv, more, stream);
+    constexpr int kStageBlocks = kC <= 2 ? 2 : 1, kOcc = kC <= 4 ? 4 : 2, kLess = kC <= 4 ? 3 : 2;
+    if (more.shared.far_blocks) {
+        if (f32) return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kLess, true, Rows::Shared>(a, parts, kv, more, stream);
+        return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kLess, false, Rows::Shared>(a, parts, kv, more, stream);
+    }
+    if (f32) return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kOcc, true, Rows::Prefix>(a, parts, kv, more, stream);
+    if constexpr (kC <= 4) {                               // of larger heads there is no tile of 128 rows that shares its operands
+        if (tile == PrefillTile::Rows128) return launch_prefill_tiles<kC, kV, kExact, 2, kStageBlocks, 4, 3, false, Rows::Prefix>(a, parts, kv, more, stream);
+    }
+    return launch_prefill_tiles<kC, kV, kExact, 1, kStageBlocks, 4, kOcc, false, Rows::Prefix>(a, parts, kv, more, stream);
 }
 
 // The sizes that those units build, and the one for a head of D dims: `go` is called with it as types.

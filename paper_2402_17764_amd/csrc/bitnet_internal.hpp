@@ -189,7 +189,7 @@ hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, 
 hipError_t launch_norm_rope_append(const void* qkv, bool bf16, bool norm, const float* q_gain, const float* k_gain, float eps, const float* inv_freq, int rotary,
                                    bool pairs, const int32_t* shift, const KvView& kv, int64_t T, int heads, void* q, hipStream_t stream);
 // attention_shared.hip, attention_weights.hip; their workspaces have the queries' bytes
-size_t attention_shared_workspace_bytes(const KvView& kv, int groups, int heads);
+size_t attention_shared_workspace_bytes(const KvView& kv, int groups, int heads, bool f32);
 hipError_t launch_attention_shared(const void* q, const KvView& kv, const int32_t* prefix_start, const int32_t* prefix_len, int groups, int heads, float scale,
                                    void* o, bool f32, void* workspace, hipStream_t stream);
 size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill, bool f32);

@@ -573,7 +573,7 @@ ENTRY(attention_decode_shared) {      // q, k_cache, v_cache, page_table, kv_len
         const int32_t* start = r.c.list<int32_t>(a[5], "prefix_start", at::kInt, groups + 1, false);
         size_t bytes = 0;
         if (a[10] == Py_None)
-            call("bitnet_attention_shared_workspace", [&] { return abi.attention_shared_workspace(&r.c.kv, groups, r.heads, &bytes); });
+            call("bitnet_attention_shared_workspace", [&] { return abi.attention_shared_workspace(&r.c.kv, groups, r.heads, r.type(), &bytes); });
         at::Tensor ws = r.c.scratch(a[10], &bytes);
         const void* qp = r.q.const_data_ptr();
         const int32_t* lp = static_cast<const int32_t*>(len.const_data_ptr());

@@ -100,8 +100,4 @@ BITNET_BOTH inline int shared_tokens(const KvView& kv, const Prefixes& p, int b,
     const SharedRows r(kv, p, sequence_of_tile(p.start, p.groups, b, 1, 1, 0));
     return b < r.first || b >= r.first + r.n ? 0 : len < r.len ? len : r.len;
 }
-// of a sequence's blocks those that hold tokens of its own, behind `shared` ones: the first, and their number
-BITNET_BOTH inline int own_first(int shared) { return shared / kKvBlock; }
-BITNET_BOTH inline int own_blocks(int len, int shared) { return shared >= len ? 0 : (len + kKvBlock - 1) / kKvBlock - own_first(shared); }
-
 }  // namespace bitnet

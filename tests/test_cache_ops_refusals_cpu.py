@@ -114,10 +114,12 @@ def test_evict_arguments():
 def test_sizes_of_workspaces():
     n = ctypes.c_size_t(0)
     f = B.load().bitnet_attention_shared_workspace
-    assert f(kv(), 1, 4, None) == NULL and f(None, 1, 4, ctypes.byref(n)) == NULL
+    assert f(kv(), 1, 4, 1, None) == NULL and f(None, 1, 4, 1, ctypes.byref(n)) == NULL
     for prefixes, heads in ((0, 4), (1 << 22, 4), (1, 3)):
-        assert f(kv(), prefixes, heads, ctypes.byref(n)) == SHAPE
-    assert f(kv(), 2, 4, ctypes.byref(n)) == 0 and n.value % 16 == 0 and 0 < n.value < 64 << 20
+        assert f(kv(), prefixes, heads, 1, ctypes.byref(n)) == SHAPE
+    assert f(kv(), 2, 4, 2, ctypes.byref(n)) == DTYPE
+    for dt in (0, 1):
+        assert f(kv(), 2, 4, dt, ctypes.byref(n)) == 0 and n.value % 16 == 0 and 0 < n.value < 64 << 20
     f = B.load().bitnet_attention_weights_workspace
     assert f(kv(), 3, 4, 0, 1, None) == NULL and f(None, 3, 4, 0, 1, ctypes.byref(n)) == NULL and f(kv(), 0, 4, 1, 1, ctypes.byref(n)) == SHAPE
     assert f(kv(), 3, 4, 0, 2, ctypes.byref(n)) == DTYPE
