@@ -212,67 +212,54 @@ __global__ __launch_bounds__(256, 2) void attention_weights_of_runs(ColumnArgs a
         float acc[kKB][8] = {};
         // Scores of 16 rows against the wave's keys, and what becomes of them.  The matrix instructions of a tile of rows run beside the exponentials of
         // the one in front of it, where the source puts them so: one after each, with a fence behind.
-        struct Scores { v4f x[kKB][2]; float2 st; };
-        auto weight = [&](const Scores& y, int u, int j) { return exp2_fast(__builtin_fmaf(y.x[u][j >> 2][j & 3], a.scale, -y.st.x)); };
-        auto scores = [&](auto with, Scores& x, const v8bf (&q)[kC], const Scores& old) {
+        struct Scores { v4f x[kKB][2]; float2 st; int pos; };
+        // adds token j of block u; masked: rows in front of it have no weight for it
+        auto add = [&](auto masked, const Scores& y, int u, int j) {
+            float p = exp2_fast(__builtin_fmaf(y.x[u][j >> 2][j & 3], a.scale, -y.st.x));
+            if (decltype(masked)::value) p = j0 + u * kKvBlock + 8 * g + j <= y.pos ? p : 0.0f;
+            acc[u][j] = __builtin_fmaf(p, y.st.y, acc[u][j]);
+        };
+        auto scores = [&](auto masked, auto with, Scores& x, const v8bf (&q)[kC], const Scores& old) {
 #pragma unroll
             for (int i = 0; i < 2 * kC * kKB; ++i) {
                 const int c = i / (2 * kKB), u = i / 2 % kKB, e = i % 2;
                 x.x[u][e] = mfma_bf16(k[u][c][e], q[c], c ? x.x[u][e] : (v4f){0, 0, 0, 0});
 #pragma unroll
                 for (int w = 0; w < 8 * kKB; ++w)
-                    if (decltype(with)::value && w * kC / 4 == i) acc[w / 8][w % 8] = __builtin_fmaf(weight(old, w / 8, w % 8), old.st.y, acc[w / 8][w % 8]);
+                    if (decltype(with)::value && w * kC / 4 == i) add(masked, old, w / 8, w % 8);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        auto flush = [&](const Scores& y) {
+        auto stage = [&](auto masked, int s) {
+            v8bf q[2][kC];
+            Scores x[2];
+            auto read = [&](int i) {
+#pragma unroll
+                for (int c = 0; c < kC; ++c) q[i & 1][c] = __builtin_bit_cast(v8bf, queries[s & 1][(i * kC + c) * 64 + lane]);
+                x[i & 1].st = stats[s & 1][i * 16 + r];
+                if (decltype(masked)::value) x[i & 1].pos = positions[s & 1][i * 16 + r];
+            };
+            read(0);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                if (i == 0) scores(masked, std::false_type(), x[0], q[0], x[0]);
+                else scores(masked, std::true_type(), x[i & 1], q[i & 1], x[1 - (i & 1)]);
+                if (i + 1 < kTiles) read(i + 1);
+            }
 #pragma unroll
             for (int u = 0; u < kKB; ++u)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[u][j] = __builtin_fmaf(weight(y, u, j), y.st.y, acc[u][j]);
+                for (int j = 0; j < 8; ++j) add(masked, x[(kTiles - 1) & 1], u, j);
         };
         publish(s0);
         __builtin_amdgcn_s_waitcnt(0);                      // the keys: waited for in the loop, they would be the next stage's loads too
         for (int s = s0; s < s1; ++s) {
             __syncthreads();
             if (s + 1 < s1) load(s + 1);
-            // positions do not fall: the first row's says whether all see all of the wave's keys
-            if (__builtin_amdgcn_readfirstlane(positions[s & 1][0]) >= j0 + kKvBlock * kKB - 1) {
-                v8bf q[2][kC];
-                Scores x[2];
-                auto read = [&](int i) {
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) q[i & 1][c] = __builtin_bit_cast(v8bf, queries[s & 1][(i * kC + c) * 64 + lane]);
-                    x[i & 1].st = stats[s & 1][i * 16 + r];
-                };
-                read(0);
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) {
-                    if (i == 0) scores(std::false_type(), x[0], q[0], x[0]);
-                    else scores(std::true_type(), x[i & 1], q[i & 1], x[1 - (i & 1)]);
-                    if (i + 1 < kTiles) read(i + 1);
-                }
-                flush(x[(kTiles - 1) & 1]);
-            } else {
-#pragma unroll 1
-                for (int i = 0; i < kTiles; ++i) {
-                    const int pos = positions[s & 1][i * 16 + r];
-                    if (!__builtin_amdgcn_ballot_w64(pos >= j0)) continue;
-                    v8bf q[kC];
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) q[c] = __builtin_bit_cast(v8bf, queries[s & 1][(i * kC + c) * 64 + lane]);
-                    Scores x;
-                    x.st = stats[s & 1][i * 16 + r];
-                    scores(std::false_type(), x, q, x);
-#pragma unroll
-                    for (int u = 0; u < kKB; ++u)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float p = j0 + u * kKvBlock + 8 * g + j <= pos ? weight(x, u, j) : 0.0f;
-                            acc[u][j] = __builtin_fmaf(p, x.st.y, acc[u][j]);
-                        }
-                }
-            }
+            // positions do not fall, and rows that there are not have -1: the first row's says whether all see all of the wave's keys
+            const int pos = positions[s & 1][lane & (kRows - 1)];
+            if (__builtin_amdgcn_readfirstlane(pos) >= j0 + kKvBlock * kKB - 1) stage(std::false_type(), s);
+            else if (__builtin_amdgcn_ballot_w64(pos >= j0)) stage(std::true_type(), s);
             if (s + 1 < s1) publish(s + 1);                 // the other half, which all waves left at the barrier
         }
         const bool whole = t.run >= t.stages;
