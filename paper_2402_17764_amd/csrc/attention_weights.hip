@@ -104,9 +104,13 @@ struct ColumnTile {
     NewTokens nt;
     // Heads side by side, so that with a multiple of eight of them a head's tiles meet on one XCD, whose L2 holds its queries; the first tiles, which most
     // rows see, first with all their shares, so that what comes last is short.
+    // 64-bit quotients are a hundred instructions each in front of the first load
+    __device__ static uint32_t each_of(int64_t task, uint32_t pairs) { return task >> 32 ? (uint32_t)(task / pairs) : (uint32_t)task / pairs; }
     __device__ ColumnTile(const ColumnArgs& a, const KvView& kv, int64_t task)
-        : h((int)(task % kv.kv_heads)), b((int)(task / kv.kv_heads % kv.B)), share((int)(task / kv.kv_heads / kv.B % a.splits)),
-          tile((int)(task / kv.kv_heads / kv.B / a.splits)), nt(kv, b, a.T) {
+        : ColumnTile(a, kv, task, (uint32_t)(kv.B * kv.kv_heads), each_of(task, (uint32_t)(kv.B * kv.kv_heads))) {}
+    __device__ ColumnTile(const ColumnArgs& a, const KvView& kv, int64_t task, uint32_t pairs, uint32_t each)
+        : h((int)((uint32_t)(task - (int64_t)each * pairs) % (uint32_t)kv.kv_heads)), b((int)((uint32_t)(task - (int64_t)each * pairs) / (uint32_t)kv.kv_heads)),
+          share((int)(each % (uint32_t)a.splits)), tile((int)(each / (uint32_t)a.splits)), nt(kv, b, a.T) {
         blocks = blocks_of(kv, b);
         blk = tile * (4 * Columns<kC>::kKB);
         j0 = blk * kKvBlock;
