@@ -27,7 +27,7 @@ struct SharedPlan {
 // are launches (us, one launch / two: 13 sequences behind 1500 tokens, 32 heads 20.4 / 25.9; 6 behind 8000, 64 heads over 8 21.4 / 24.7; 16 behind 16000
 // 36.1 / 35.2; 30 behind 16000, 28 over 4 41.3 / 40.3; 48 behind 24000, 64 over 8 127 / 112).  Two launches, and 256 rows: tiles of 128, which halve what comes
 // through LDS (the last one 103; 30 behind 16000 43.6).  The shared keys are split until there are two workgroups for each CU, a sequence's own until there
-// are four, with 256 tokens each or more (48 behind 24000, own ones in a workgroup each: 46 us for them, split 39; shared ones to three workgroups a CU 110).
+// are four or five, with 256 tokens each or more (48 behind 24000, own ones in a workgroup each: 46 us for them, split 39; shared ones to three workgroups a CU 110).
 SharedPlan shared_plan(const KvView& kv, int groups, int heads, bool f32) {
     const int group = heads / kv.kv_heads;
     const int64_t capacity = (int64_t)kv.max_blocks * kKvBlock, rows = ceil_div((int64_t)kv.B * group, groups), most = ceil_div(capacity, 256);
@@ -41,7 +41,7 @@ SharedPlan shared_plan(const KvView& kv, int groups, int heads, bool f32) {
         return (int)(n < 1 ? 1 : n > kMostSplits / 2 ? kMostSplits / 2 : n);
     };
     p.near = splits(p.near_tiles * kv.kv_heads, 512);
-    p.far = splits((int64_t)kv.B * kv.kv_heads * p.far_tiles, 1024);
+    p.far = splits((int64_t)kv.B * kv.kv_heads * p.far_tiles, p.apart ? 1280 : 1024);
     p.least_near = 256 / kStageTokens;
     p.least_far = 256 / (p.apart ? kKvBlock : kStageTokens);
     return p;
