@@ -592,7 +592,8 @@ bitnet_status bitnet_norm_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype
  *                  that the table row of the run's first sequence names; the others' rows are read for the tokens behind them alone, so a
  *                  page that the prefix fills in part may be another one in each row.  A sequence of fewer tokens sees those it has.
  *   prefixes       at least 1, prefixes*heads < 2^22 (BITNET_ERR_SHAPE otherwise); runs may be empty
- *   workspace      device memory, 16-byte aligned, of the bitnet_attention_shared_workspace() bytes or more (BITNET_ERR_WORKSPACE otherwise; it is needed here)
+ *   workspace      device memory, 16-byte aligned, of the bitnet_attention_shared_workspace() bytes for that type of result or more (BITNET_ERR_WORKSPACE
+ *                  otherwise; it is needed here): contents are scratch; calls that share it must not overlap
  *   Weights enter their product as in bitnet_attention_prefill (of a BF16 result's own tokens as in bitnet_attention_decode, for groups of many rows).
  *   kv->q_start is not read.
  */
@@ -604,9 +605,11 @@ bitnet_status bitnet_attention_decode_shared(const void* q, const bitnet_kv* kv,
  * bitnet_attention_decode and bitnet_attention_prefill that also add up what weight each cached token has had:
  *   weights[b][h][j] += sum over the call's rows of sequence b, and the query heads that read key-value head h, of the softmax weight of token j.
  *   weights         [B][kv_heads] rows of weights_stride floats (device), weights_stride >= max_pages*page_tokens.  Tokens 0 .. kv_len[b]-1 are updated; the
- *                   call's own new ones begin with nothing, whatever stood there.  Fp32, from weights that are not rounded; sums in a fixed order.
- *   workspace       device memory, 16-byte aligned, of the bitnet_attention_weights_workspace() bytes or more (BITNET_ERR_WORKSPACE otherwise; it is needed
- *                   here): for single tokens 4 bytes for each query head and token that the tables have room for, for runs 8 for each row and head
+ *                   call's own new ones begin with nothing, whatever stood there; sequences without rows in the call are left alone.  Fp32, from weights
+ *                   that are not rounded; sums in a fixed order.
+ *   workspace       device memory, 16-byte aligned, of the bitnet_attention_weights_workspace() bytes for that type of result or more (BITNET_ERR_WORKSPACE
+ *                   otherwise; it is needed here): contents are scratch; calls that share it must not overlap.  For single tokens it holds 4 bytes for each
+ *                   query head and token that the tables have room for, for runs 8 for each row and head, and what few rows on long sequences take
  */
 bitnet_status bitnet_attention_weights_workspace(const bitnet_kv* kv, int64_t T, int64_t heads, int prefill, bitnet_dtype o_dtype, size_t* bytes);
 bitnet_status bitnet_attention_decode_weights(const void* q, const bitnet_kv* kv, int64_t heads, float scale, void* o, bitnet_dtype o_dtype, float* weights,

@@ -29,6 +29,8 @@ struct SingleMore {
     Prefixes prefixes;
     int first, pitch;                  // Own
     float* scores;                     // Scored: [B][heads][max_blocks * 32], what q . k is, -inf for no key
+    float* weights;                    // Scored, where a workgroup has all heads and keys of a row: what it adds the weights to itself, or NULL
+    int64_t stride;
 };
 
 // A row is 16 query heads (or what a group has left) of one key-value head of one sequence.  Its blocks are dealt out to up to
@@ -219,6 +221,38 @@ __global__ __launch_bounds__(64 * kW, kC <= 4 ? 2 : 1) void attention_decode_row
             }
         }
         __syncthreads();
+    }
+    // The row's scores, written by this workgroup in front of those barriers, into weights: four tokens a thread, all heads one behind the other.
+    if constexpr (kDo == Single::Scored) {
+        if (!more.weights) return;
+        if (threadIdx.x < 16) {
+            float top = kMinusInf, total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kW; ++w) top = fmaxf(top, maxima[w * 16 + threadIdx.x]);
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                const float mw = maxima[w * 16 + threadIdx.x];
+                total += mw == kMinusInf ? 0.0f : totals[w * 16 + threadIdx.x] * exp2_fast((mw - top) * a.scale);
+            }
+            sums[2 * threadIdx.x] = top == kMinusInf ? 0.0f : top * a.scale;
+            sums[2 * threadIdx.x + 1] = total > 0.0f ? 1.0f / total : 0.0f;
+        }
+        __syncthreads();
+        const int64_t capacity = (int64_t)kv.max_blocks * kKvBlock;
+        const float* from = more.scores + ((int64_t)b * a.heads + head0) * capacity;
+        float* to = more.weights + ((int64_t)b * kv.kv_heads + h) * more.stride;
+        for (int64_t pos = 4 * threadIdx.x; pos < len; pos += 4 * 64 * kW) {
+            v4f sum = {0, 0, 0, 0};
+#pragma unroll 4
+            for (int e = 0; e < columns; ++e) {
+                const v4f s = *reinterpret_cast<const v4f*>(from + e * capacity + pos);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(exp2_fast(__builtin_fmaf(s[i], a.scale, -sums[2 * e])), sums[2 * e + 1], sum[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (pos + i < len) to[pos + i] = (pos + i == len - 1 ? 0.0f : to[pos + i]) + sum[i];      // the call's own token begins with nothing
+        }
     }
 }
 

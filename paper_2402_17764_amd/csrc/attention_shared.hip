@@ -134,7 +134,7 @@ hipError_t launch_attention_shared(const void* q, const KvView& kv, const int32_
     if (e != hipSuccess) return e;
     if (plan.apart) {
         const DecodeArgs da{a.q, nullptr, by, heads, group, (int)plan.far_tiles};
-        const SingleMore more{l.prefixes, plan.near, plan.near + plan.far, nullptr};
+        const SingleMore more{l.prefixes, plan.near, plan.near + plan.far, nullptr, nullptr, 0};
         Parts own = parts;
         own.splits = plan.far;
         own.least = plan.least_far;

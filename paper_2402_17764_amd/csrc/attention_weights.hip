@@ -19,7 +19,9 @@ struct WeightsArgs {
 };
 constexpr int kChunk = 1024;
 
-// Joins the rows that several workgroups shared, one to a workgroup, then turns chunks of scores into weights, four tokens a thread.
+// Joins the rows that several workgroups shared, one to a workgroup, then turns chunks of scores into weights, four tokens a thread.  Bound by memory: three
+// sequences of 20000 to 49152 tokens, 64 heads over 8, 31 MB of scores in 9.5 us.  What scores cost more is that they are written beside the stream of the
+// cache (there 80 us with them, 66 without; with streaming stores 85).
 template <bool kF32>
 __global__ __launch_bounds__(256) void attention_weights_of_tokens(void* o, WeightsArgs a, Parts parts, KvView kv) {
     __shared__ JoinRoom room;
@@ -150,6 +152,10 @@ __device__ inline v4u settle_dims(v4u w, int d0, int D) {
 // A workgroup takes a tile of keys and a run of the rows that see any of it, which come through LDS a stage at a time for its four waves, the next
 // stage requested while one is worked on.  Scores are products of keys (down) and queries (across), so that a lane sums up eight tokens of a block for
 // its queries; the lanes of a group meet at the end.
+//
+// Bound by exponentials and matrix instructions in turn (counters on a chunk of 1024 tokens behind 15000, 64 heads over 8: the matrix pipe 37 % busy, the vector
+// pipe 59 %; 285 us, 0.91 PFLOP/s), of short runs by what a workgroup begins with and by its rows' way from memory, one stage ahead (a prompt of 2048 tokens, 40
+// heads: 39 us, 0.55 PFLOP/s).  Rows straight from memory to each wave's registers, without LDS, took 64 us there: four times as many bytes through the L2.
 template <int kC, bool kExact>
 __global__ __launch_bounds__(256, 2) void attention_weights_of_runs(ColumnArgs a, KvView kv) {
     using Shape = Columns<kC>;
@@ -366,14 +372,17 @@ hipError_t launch_attention_decode_weights(const void* q, const KvView& kv, int 
     const Parts parts(workspace, rows, plan.splits.n, plan.splits.least, kv.D);
     const DecodeArgs a{static_cast<const uint16_t*>(q), o, by, heads, group, (int)ceil_div(group, 16)};
     float* scores = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.parts);
-    const SingleMore more{{}, 0, 0, scores};
+    // Rows that one workgroup has are weighed by it, in the one launch (us, two launches / one: a sequence of 700 tokens, 24 heads of 64 10.8 / 8.5; 29 of up to
+    // 500, 32 heads 31.4 / 28.6, of up to 4000 190 / 194; 40 of up to 2000, 64 heads over 8 58 / 53).
+    const bool alone = plan.splits.n == 1 && a.column_tiles == 1;
+    const SingleMore more{{}, 0, 0, scores, alone ? weights : nullptr, stride};
     const hipError_t e = for_head_size(kv.D, [&](auto c, auto v, auto exact) {
         const dim3 grid((unsigned)((int64_t)kv.B * kv.kv_heads * a.column_tiles), parts.splits);
         if (f32) attention_decode_rows<c.value, v.value, exact.value, true, 4, Single::Scored><<<grid, 256, 0, stream>>>(a, parts, kv, more);
         else attention_decode_rows<c.value, v.value, exact.value, false, 4, Single::Scored><<<grid, 256, 0, stream>>>(a, parts, kv, more);
         return hipGetLastError();
     });
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || alone) return e;
     const int chunks = (int)ceil_div((int64_t)kv.max_blocks * kKvBlock, kChunk), joins = parts.splits > 1 ? (int)rows : 0;
     const int64_t tasks = (int64_t)kv.B * kv.kv_heads * chunks;
     const WeightsArgs w{scores, weights, stride, tasks, by, heads, group, chunks, joins};
