@@ -594,7 +594,7 @@ bitnet_status bitnet_norm_rope_kv_append(const void* qkv, bitnet_dtype qkv_dtype
  *   prefixes       at least 1, prefixes*heads < 2^22 (BITNET_ERR_SHAPE otherwise); runs may be empty
  *   workspace      device memory, 16-byte aligned, of the bitnet_attention_shared_workspace() bytes for that type of result or more (BITNET_ERR_WORKSPACE
  *                  otherwise; it is needed here): contents are scratch; calls that share it must not overlap
- *   Weights enter their product as in bitnet_attention_prefill (of a BF16 result's own tokens as in bitnet_attention_decode, for groups of many rows).
+ *   Weights enter their product as in bitnet_attention_decode, whatever runs there are.
  *   kv->q_start is not read.
  */
 bitnet_status bitnet_attention_shared_workspace(const bitnet_kv* kv, int64_t prefixes, int64_t heads, bitnet_dtype o_dtype, size_t* bytes);

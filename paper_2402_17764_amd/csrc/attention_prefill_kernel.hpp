@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     // stage of two blocks the scores of the second with the weights of the first, the values of the first with the weights of the second (with
     // one block, the other waves' matrix instructions fill that time).  Operands are read from LDS kAhead fragments ahead of their products,
     // keys and values in one sequence.
-    constexpr int kParts = kF32 ? 3 : kOf == Rows::Shared ? 2 : 1, kAhead = 3, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
+    constexpr int kParts = kF32 ? 3 : of_groups(kOf) ? 2 : 1, kAhead = 3, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
     auto take = [&](auto masked_, const char* keys, const char* values, int j0, const bool (&known)[kU]) {
         constexpr bool kMasked = decltype(masked_)::value;
         v4f sc[kU][2][kNT];

@@ -24,9 +24,9 @@ struct SharedPlan {
     int near, least_near, far, least_far;
 };
 // Groups of up to 128 rows (of a key-value head, on average) take one launch for both: a few rows leave its matrix instructions to spare, and what counts
-// are launches (us, one launch / two: 13 sequences behind 1500 tokens, 32 heads 20.4 / 25.9; 6 behind 8000, 64 heads over 8 21.4 / 24.7; 16 behind 16000
-// 36.1 / 35.2; 30 behind 16000, 28 over 4 41.3 / 40.3; 48 behind 24000, 64 over 8 127 / 112).  Two launches, and 256 rows: tiles of 128, which halve what comes
-// through LDS (the last one 103; 30 behind 16000 43.6).  The shared keys are split until there are two workgroups for each CU, a sequence's own until there
+// are launches (us, one launch / two: 13 sequences behind 1500 tokens, 32 heads 20.1 / 25.5; 6 behind 8000, 64 heads over 8 22.5 / 24.7; 16 behind 16000
+// 37.2 / 38.7, 20 45.2 / 40.5; 30 behind 16000, 28 over 4 42.5 / 41.0; 48 behind 24000, 64 over 8 135 / 115).  Two launches, and 256 rows: tiles of 128, which halve what comes
+// through LDS (the last one 110; 30 behind 16000, which has 210, 44.8).  The shared keys are split until there are two workgroups for each CU, a sequence's own until there
 // are four or five, with 256 tokens each or more (48 behind 24000, own ones in a workgroup each: 46 us for them, split 39; shared ones to three workgroups a CU 110).
 SharedPlan shared_plan(const KvView& kv, int groups, int heads, bool f32) {
     const int group = heads / kv.kv_heads;
