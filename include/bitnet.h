@@ -602,7 +602,8 @@ bitnet_status bitnet_attention_decode_shared(const void* q, const bitnet_kv* kv,
                                              int64_t heads, float scale, void* o, bitnet_dtype o_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * bitnet_attention_decode and bitnet_attention_prefill that also add up what weight each cached token has had:
+ * bitnet_attention_decode and bitnet_attention_prefill that also add up what weight each cached token has had (weights enter the product with the
+ * values as the sum of two bf16 at least, whichever of them it is):
  *   weights[b][h][j] += sum over the call's rows of sequence b, and the query heads that read key-value head h, of the softmax weight of token j.
  *   weights         [B][kv_heads] rows of weights_stride floats (device), weights_stride >= max_pages*page_tokens.  Tokens 0 .. kv_len[b]-1 are updated; the
  *                   call's own new ones begin with nothing, whatever stood there; sequences without rows in the call are left alone.  Fp32, from weights

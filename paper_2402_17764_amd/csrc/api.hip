@@ -707,7 +707,7 @@ bitnet_status bitnet_attention_weights_workspace(const bitnet_kv* kv, int64_t T,
     const bitnet_status st = kv_view(kv, T, heads, &view);
     if (st != BITNET_OK) return st;
     if (o_dtype != BITNET_F32 && o_dtype != BITNET_BF16) return BITNET_ERR_DTYPE;
-    *bytes = bitnet::attention_weights_workspace_bytes(view, T, (int)heads, prefill != 0, o_dtype == BITNET_F32);
+    *bytes = bitnet::attention_weights_workspace_bytes(view, T, (int)heads, prefill != 0);
     return BITNET_OK;
 }
 
@@ -723,7 +723,7 @@ bitnet_status bitnet_attention_decode_weights(const void* q, const bitnet_kv* kv
     bitnet_status st = attention_checked(q, kv, kv ? kv->sequences : 1, heads, scale, o, o_dtype, workspace, &view);
     if (st == BITNET_OK) st = weights_checked(view, weights, weights_stride);
     if (st != BITNET_OK) return st;
-    if (workspace_bytes < bitnet::attention_weights_workspace_bytes(view, view.B, (int)heads, false, o_dtype == BITNET_F32)) return BITNET_ERR_WORKSPACE;
+    if (workspace_bytes < bitnet::attention_weights_workspace_bytes(view, view.B, (int)heads, false)) return BITNET_ERR_WORKSPACE;
     return from_hip(bitnet::launch_attention_decode_weights(q, view, (int)heads, scale, o, o_dtype == BITNET_F32, weights, weights_stride, workspace,
                                                             static_cast<hipStream_t>(stream)));
 }
@@ -736,7 +736,7 @@ bitnet_status bitnet_attention_prefill_weights(const void* q, const bitnet_kv* k
     if (st == BITNET_OK) st = weights_checked(view, weights, weights_stride);
     if (st != BITNET_OK) return st;
     if (!view.q_start) return BITNET_ERR_NULL;
-    if (workspace_bytes < bitnet::attention_weights_workspace_bytes(view, T, (int)heads, true, o_dtype == BITNET_F32)) return BITNET_ERR_WORKSPACE;
+    if (workspace_bytes < bitnet::attention_weights_workspace_bytes(view, T, (int)heads, true)) return BITNET_ERR_WORKSPACE;
     return from_hip(bitnet::launch_attention_prefill_weights(q, view, T, (int)heads, scale, o, o_dtype == BITNET_F32, weights, weights_stride, workspace,
                                                              workspace_bytes, static_cast<hipStream_t>(stream)));
 }

@@ -103,8 +103,9 @@ __device__ inline void settle_query(v8bf (&f)[kC], int g, int D) {
 // cost is a product of values each: of single tokens, which wait for memory, next to nothing (us, one / two / three: 29 sequences of up to 4096
 // tokens, 32 heads of 128 160 / 164 / 162, 64 heads over 8, 20000 to 49000 tokens 73.6 / 74.2 / 74.5, 1000 tokens 8.4 / 8.6 / 8.8), of
 // runs a quarter of the time or more (40 heads of 128, 2048 tokens 57 / 73, 64 heads over 8, 1024 behind 15000 445 / 666).  So
-// decode takes two for a bf16 result, over shared prefixes too (where one would be 98 us instead of 111 for 48 sequences behind 24000 tokens), and prefill
-// one; all take three for fp32.
+// decode takes two for a bf16 result and prefill one, and both take three for fp32.  Over shared prefixes, and where weights of tokens are added up, whose
+// state of a row is that of weights as they are, runs take two as well (one would be 98 us instead of 111 for 48 sequences behind 24000 tokens, 101 instead of 113
+// for a prompt of 2048 tokens, 40 heads).
 template <int kParts>
 __device__ inline void weights_pair(v8bf* w, int j, float p0, float p1) {
 #pragma unroll
@@ -198,10 +199,9 @@ struct JoinArgs {
     float scale;                       // of the softmax, times log2 e
     int heads, group, T, rows_a_tile;
 };
-// Where rows leave their softmax states, m and l of weights that are not rounded.
+// Where rows leave their softmax states, m and l.
 struct KeptRows {
     float* state = nullptr;            // [rows][2]
-    float* totals = nullptr;           // of the splits, as Parts' places: l of weights that are not rounded; NULL where Parts' l is that already
 };
 hipError_t launch_attention_join(const JoinArgs& a, const Parts& parts, const KvView& kv, bool f32, hipStream_t stream, const KeptRows& keep = KeptRows());
 

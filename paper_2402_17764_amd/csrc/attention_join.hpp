@@ -21,16 +21,14 @@ __device__ inline float wave_sum(float v) {
 
 // LDS of a workgroup that joins a row
 struct JoinRoom {
-    float weights[kMostSplits], totals[4], tops[4], others[4];
+    float weights[kMostSplits], totals[4], tops[4];
     v4f sums[4][64];
 };
-struct JoinState { float top, total, other; };             // m and l of the row, and the sum over `others`
+struct JoinState { float top, total; };                    // m and l of the row
 
 // Joins the `n` splits of row `row`, of which the first `near` stand at places place0, place0 + 1, ... and the others from place0 + far on.
-// `others`: another l of each place, which is summed up too, or NULL.
 template <bool kF32>
-__device__ inline JoinState join_row(JoinRoom& room, const Parts& parts, int64_t place0, int n, int near, int far, float scale, int D, void* o, int64_t row,
-                                     const float* others = nullptr) {
+__device__ inline JoinState join_row(JoinRoom& room, const Parts& parts, int64_t place0, int n, int near, int far, float scale, int D, void* o, int64_t row) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), dim = 4 * lane;
     auto place = [&](int s) { return place0 + (s < near ? s : far + (s - near)); };
     auto sums_of = [&](int s) {
@@ -53,10 +51,6 @@ __device__ inline JoinState join_row(JoinRoom& room, const Parts& parts, int64_t
     room.weights[threadIdx.x] = w;
     l = wave_sum(l * w);
     if (lane == 0) room.totals[wave] = l;
-    if (others) {
-        const float l2 = wave_sum((int)threadIdx.x < n ? others[place(threadIdx.x)] * w : 0.0f);
-        if (lane == 0) room.others[wave] = l2;
-    }
     __syncthreads();
     v4f x = {0, 0, 0, 0};
 #pragma unroll 4
@@ -64,13 +58,12 @@ __device__ inline JoinState join_row(JoinRoom& room, const Parts& parts, int64_t
     room.sums[wave][lane] = x;
     __syncthreads();
     const float total = (room.totals[0] + room.totals[1]) + (room.totals[2] + room.totals[3]);
-    const float other = others ? (room.others[0] + room.others[1]) + (room.others[2] + room.others[3]) : total;
-    if (wave != 0 || dim >= D) return {top, total, other};
+    if (wave != 0 || dim >= D) return {top, total};
     x = (room.sums[0][lane] + room.sums[1][lane]) + (room.sums[2][lane] + room.sums[3][lane]);
     const float inv = total > 0.0f ? 1.0f / total : 0.0f;
     const float y[4] = {finite_or_nan(x[0], inv), finite_or_nan(x[1], inv), finite_or_nan(x[2], inv), finite_or_nan(x[3], inv)};
     store4<kF32>(o, row * D, dim, D, y);
-    return {top, total, other};
+    return {top, total};
 }
 
 }  // namespace bitnet

@@ -35,18 +35,14 @@ size_t attention_prefill_workspace_bytes(const KvView& kv, int64_t T, int heads)
     return Parts::bytes(T * heads, prefill_plan(kv, T, heads).splits, kv.D);
 }
 
-// `keep`: rows leave their softmax states there (its totals are set here), if it names a place
+// `keep`: rows leave their softmax states there, if it names a place
 static hipError_t launch_runs(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, KeptRows keep, void* workspace,
                               size_t workspace_bytes, hipStream_t stream) {
     const float by = scale * 1.44269504f;
     const PrefillArgs a{static_cast<const uint16_t*>(q), o, by, fminf(kSlack / by, 3e38f), heads, heads / kv.kv_heads, (int)T, 0};
     const PrefillPlan plan = prefill_plan(kv, T, heads);
-    const size_t bytes = Parts::bytes(T * heads, plan.splits, kv.D);
     Parts parts;
-    if (plan.splits > 1 && workspace_bytes >= (keep.state ? attention_prefill_kept_bytes(kv, T, heads, f32) : bytes)) {
-        parts = Parts(workspace, T * heads, plan.splits, plan.least, kv.D);
-        if (keep.state && !f32) keep.totals = reinterpret_cast<float*>(static_cast<char*>(workspace) + bytes);
-    }
+    if (plan.splits > 1 && workspace_bytes >= Parts::bytes(T * heads, plan.splits, kv.D)) parts = Parts(workspace, T * heads, plan.splits, plan.least, kv.D);
     const hipError_t e = for_head_size(kv.D, [&](auto c, auto v, auto exact) {
         if (keep.state) return launch_prefill_kept<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, RowsMore{keep, {}}, stream);
         return launch_prefill<c.value, v.value, exact.value>(plan.tile, a, parts, kv, f32, stream);
@@ -60,10 +56,6 @@ hipError_t launch_attention_prefill(const void* q, const KvView& kv, int64_t T, 
     return launch_runs(q, kv, T, heads, scale, o, f32, {}, workspace, workspace_bytes, stream);
 }
 
-size_t attention_prefill_kept_bytes(const KvView& kv, int64_t T, int heads, bool f32) {
-    const int splits = prefill_plan(kv, T, heads).splits;
-    return Parts::bytes(T * heads, splits, kv.D) + (splits < 2 || f32 ? 0 : ((size_t)(T * heads * splits) * 4 + 15) / 16 * 16);
-}
 hipError_t launch_attention_prefill_kept(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, const KeptRows& keep,
                                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
     return launch_runs(q, kv, T, heads, scale, o, f32, keep, workspace, workspace_bytes, stream);

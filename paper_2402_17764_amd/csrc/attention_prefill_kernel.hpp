@@ -24,8 +24,7 @@ struct PrefillArgs {
     int tiles;                         // of the launch, per key-value head
 };
 
-// Whose rows a launch takes: runs of new tokens, causal; the same, leaving each row's softmax state (of weights as they are, not as they are rounded)
-// for the weights of the keys; or the single new tokens of sequences that share their first tokens, as parts of rows: over those of a group alone, its
+// Whose rows a launch takes: runs of new tokens, causal; the same, leaving each row's softmax state for the weights of the keys; or the single new tokens of sequences that share their first tokens, as parts of rows: over those of a group alone, its
 // sequences in place of new tokens, or over what each sequence has behind them as well.
 enum class Rows { Causal, Kept, Prefix, Shared };
 constexpr bool of_groups(Rows r) { return r == Rows::Prefix || r == Rows::Shared; }
@@ -209,8 +208,6 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 
     v4f acc[kNT][kV];
     float m[kNT], base[kNT], l[kNT];                                       // base: m times scale, or 0; l: of this lane's tokens
-    constexpr bool kBoth = kOf == Rows::Kept && !kF32;                     // another sum, of weights that are not rounded
-    [[maybe_unused]] float whole_l[kNT] = {};
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         m[n] = kMinusInf;
@@ -224,7 +221,7 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
     // stage of two blocks the scores of the second with the weights of the first, the values of the first with the weights of the second (with
     // one block, the other waves' matrix instructions fill that time).  Operands are read from LDS kAhead fragments ahead of their products,
     // keys and values in one sequence.
-    constexpr int kParts = kF32 ? 3 : of_groups(kOf) ? 2 : 1, kAhead = 3, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
+    constexpr int kParts = kF32 ? 3 : kOf == Rows::Causal ? 1 : 2, kAhead = 3, kKeys = 2 * kC;       // kKeys: fragments of a block's keys; it has kV of values
     auto take = [&](auto masked_, const char* keys, const char* values, int j0, const bool (&known)[kU]) {
         constexpr bool kMasked = decltype(masked_)::value;
         v4f sc[kU][2][kNT];
@@ -243,7 +240,6 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                 const float p1 = exp2_fast(__builtin_fmaf(sc[u][j >> 2][n][(j & 3) + 1], a.scale, -base[n]));
                 weights_pair<kParts>(w[u][n], j, p0, p1);
                 l[n] = kParts > 1 ? l[n] + p0 + p1 : add_rounded(l[n], w[u][n][0], j);
-                if constexpr (kBoth) whole_l[n] += p0 + p1;
             }
         };
         auto scores = [&](int u, int with) {
@@ -306,7 +302,6 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
                     m[n] = now;
                     base[n] = now == kMinusInf ? 0.0f : now * a.scale;
                     l[n] *= by;
-                    if constexpr (kBoth) whole_l[n] *= by;
 #pragma unroll
                     for (int i = 0; i < kV; ++i) acc[n][i] *= by;
                     if (u > 0)
@@ -406,8 +401,6 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
 #pragma unroll
     for (int n = 0; n < kNT; ++n) {
         const float total = groups_sum(l[n]), inv = total > 0.0f ? 1.0f / total : 0.0f;
-        [[maybe_unused]] float kept = total;
-        if constexpr (kBoth) kept = groups_sum(whole_l[n]);
         if (out_row[n] < 0) continue;
         const int64_t place = (int64_t)out_row[n] * parts.splits + split;
         const bool whole = !of_groups(kOf) && run >= all_stages;
@@ -425,12 +418,11 @@ __global__ __launch_bounds__(64 * kW, kOcc) void attention_prefill_tiles(Prefill
         if (!whole && g == 0) {
             parts.state[2 * place] = m[n];
             parts.state[2 * place + 1] = total;
-            if constexpr (kBoth) more.keep.totals[place] = kept;
         }
         if constexpr (kOf == Rows::Kept)
             if (whole && g == 0) {
                 more.keep.state[2 * (int64_t)out_row[n]] = m[n];
-                more.keep.state[2 * (int64_t)out_row[n] + 1] = kept;
+                more.keep.state[2 * (int64_t)out_row[n] + 1] = total;
             }
     }
 #endif
@@ -493,8 +485,7 @@ hipError_t launch_prefill_shared(PrefillTile tile, const PrefillArgs& a, const P
     template hipError_t launch_prefill_kept<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, const RowsMore&, hipStream_t); \
     template hipError_t launch_prefill_shared<kC_, kV_, kE_>(PrefillTile, const PrefillArgs&, const Parts&, const KvView&, bool, const RowsMore&, hipStream_t);
 
-// Runs of rows whose softmax states are kept.  keep.totals is taken from the workspace: attention_prefill_kept_bytes.
-size_t attention_prefill_kept_bytes(const KvView& kv, int64_t T, int heads, bool f32);
+// Runs of rows whose softmax states are kept; the workspace is that of runs.
 hipError_t launch_attention_prefill_kept(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, const KeptRows& keep, void* workspace,
                                          size_t workspace_bytes, hipStream_t stream);
 

@@ -345,8 +345,8 @@ constexpr int64_t kMostBlocks = 1 << 20;                   // of a launch that l
 
 // Of runs: the rows' states, the parts of tiles of keys, and what the attention takes.
 struct RunsPlan { size_t states, parts, attention; };
-static RunsPlan runs_plan(const KvView& kv, int64_t T, int heads, bool f32) {
-    RunsPlan p{((size_t)(T * heads) * 8 + 15) / 16 * 16, 0, attention_prefill_kept_bytes(kv, T, heads, f32)};
+static RunsPlan runs_plan(const KvView& kv, int64_t T, int heads) {
+    RunsPlan p{((size_t)(T * heads) * 8 + 15) / 16 * 16, 0, attention_prefill_workspace_bytes(kv, T, heads)};
     (void)for_head_size(kv.D, [&](auto c, auto, auto) {
         p.parts = columns_plan<c.value>(kv, T, heads / kv.kv_heads).bytes;
         return hipSuccess;
@@ -354,9 +354,9 @@ static RunsPlan runs_plan(const KvView& kv, int64_t T, int heads, bool f32) {
     return p;
 }
 
-size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill, bool f32) {
+size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill) {
     if (prefill) {
-        const RunsPlan p = runs_plan(kv, T, heads, f32);
+        const RunsPlan p = runs_plan(kv, T, heads);
         return p.states + p.parts + p.attention;
     }
     const TokensPlan p = tokens_plan(kv, heads);
@@ -394,7 +394,7 @@ hipError_t launch_attention_decode_weights(const void* q, const KvView& kv, int 
 
 hipError_t launch_attention_prefill_weights(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, float* weights, int64_t stride,
                                             void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    const RunsPlan plan = runs_plan(kv, T, heads, f32);
+    const RunsPlan plan = runs_plan(kv, T, heads);
     char* at = static_cast<char*>(workspace);
     KeptRows keep;
     keep.state = reinterpret_cast<float*>(at);

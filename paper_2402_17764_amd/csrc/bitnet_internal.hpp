@@ -192,7 +192,7 @@ hipError_t launch_norm_rope_append(const void* qkv, bool bf16, bool norm, const 
 size_t attention_shared_workspace_bytes(const KvView& kv, int groups, int heads, bool f32);
 hipError_t launch_attention_shared(const void* q, const KvView& kv, const int32_t* prefix_start, const int32_t* prefix_len, int groups, int heads, float scale,
                                    void* o, bool f32, void* workspace, hipStream_t stream);
-size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill, bool f32);
+size_t attention_weights_workspace_bytes(const KvView& kv, int64_t T, int heads, bool prefill);
 hipError_t launch_attention_decode_weights(const void* q, const KvView& kv, int heads, float scale, void* o, bool f32, float* weights, int64_t stride,
                                            void* workspace, hipStream_t stream);
 hipError_t launch_attention_prefill_weights(const void* q, const KvView& kv, int64_t T, int heads, float scale, void* o, bool f32, float* weights, int64_t stride,

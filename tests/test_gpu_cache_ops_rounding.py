@@ -45,3 +45,18 @@ def test_decode_weights(gpu_lib, lens, D):
     y = host(gpu_lib.attention_decode_weights(dev16(q), batch.k, batch.v, dev(batch.table), dev(lens), acc, y_dtype=gpu_lib.BF16))
     for b, n in enumerate(lens):
         rounded_once(y[b], q[b], *batch.cache.get(batch.table[b], n), n)
+
+
+# tiles of 64 rows; rows that workgroups share; tiles of 128 rows, of a chunk behind others and of a prompt in a table that has room for more
+@pytest.mark.parametrize("sizes,heads,kv_heads,per", [([(0, 300), (45, 1), (130, 70)], 4, 2, None), ([(3000, 5)], 4, 2, None), ([(4500, 1030)], 64, 8, None), ([(0, 300)], 256, 32, 20)])
+@pytest.mark.parametrize("D", DIMS)
+def test_prefill_weights(gpu_lib, sizes, heads, kv_heads, per, D):
+    lens, starts = [o + n for o, n in sizes], np.cumsum([0] + [n for _, n in sizes])
+    batch = Batch(lens, 64, kv_heads, D, 93, per)
+    T = int(starts[-1])
+    q, acc = batch.queries(T, heads, D), torch.zeros((len(lens), kv_heads, batch.per * 64), device="cuda")
+    y = host(gpu_lib.attention_prefill_weights(dev16(q), batch.k, batch.v, dev(batch.table), dev(lens), dev(starts), acc, y_dtype=gpu_lib.BF16))
+    for b, (old, n) in enumerate(sizes):
+        k, v, there = batch.cache.get(batch.table[b], lens[b])
+        for i in sorted({0, n - 1} | set(int(i) for i in batch.rng.integers(0, n, 5))):
+            rounded_once(y[starts[b] + i], q[starts[b] + i], k, v, there & (np.arange(lens[b]) <= old + i), (b, i))
