@@ -1,8 +1,8 @@
 // Norms of queries and keys head by head, rotary positions and the paged cache, in one pass over the rows of a merged Q | K | V product.
 //
 // A head x of D dims becomes y = x r gain, r = 1 / sqrt(mean(x^2) + eps), and y is turned by its position as in rope_append.hip; the position
-// is the token's place in the cache plus its sequence's shift.  Squares are summed in 32 bits, or in 64 where 32 cannot hold them; products and turns are
-// 32 bits wide, and the result is rounded once, to the cache's bf16.
+// is the token's place in the cache plus its sequence's shift.  Squares are summed in 64 bits, which hold them whatever the head's size is; products and
+// turns are 32 bits wide, and the result is rounded once, to the cache's bf16.
 #include "rope_slots.hpp"
 
 namespace bitnet {
@@ -17,16 +17,7 @@ struct NormShape {
     int norm;                          // 0: heads are turned as they are
 };
 
-// 1 / sqrt(mean + eps).  A sum of squares that 32 bits hold with room on both sides takes the 32-bit instruction (within 2^-23); the others are summed up
-// again in 64 bits, with the 64-bit instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is.
-__device__ inline bool in_range(float sum) { return sum > 1e-30f && sum < 1e37f; }
-__device__ inline float head_scale(float sum, float inv_d, float eps) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_d, eps));
-#else
-    return 0.0f;
-#endif
-}
+// 1 / sqrt(mean + eps): the 64-bit instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is.
 __device__ inline float head_scale(double sum, double inv_d, float eps) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const double a = __builtin_fma(sum, inv_d, (double)eps);
@@ -38,29 +29,19 @@ __device__ inline float head_scale(double sum, double inv_d, float eps) {
 #endif
 }
 
-template <bool kBf16, typename Sum>
-__device__ inline Sum squares_of(const Eight<kBf16>& v, int count) {
+template <bool kBf16>
+__device__ inline double squares_of(const Eight<kBf16>& v, int count) {
     float x[8];
     floats_of<kBf16>(x, v);
-    Sum s = 0;
+    double s = 0.0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const Sum y = e < count ? (Sum)x[e] : (Sum)0;
-        if constexpr (sizeof(Sum) == 4) s = __builtin_fmaf(y, y, s);
-        else s = __builtin_fma(y, y, s);
+        const double y = e < count ? (double)x[e] : 0.0;
+        s = __builtin_fma(y, y, s);
     }
     return s;
 }
 // the sum over kLanes neighbouring lanes
-template <int kLanes>
-__device__ inline float lanes_sum(float v) {
-    v += dpp_f32<0xB1>(v);
-    v += dpp_f32<0x4E>(v);
-    v += dpp_f32<0x141>(v);
-    if (kLanes >= 16) v += dpp_f32<0x140>(v);
-    if (kLanes >= 32) v += __shfl_xor(v, 16);
-    return v;
-}
 template <int kLanes>
 __device__ inline double lanes_sum(double v) {
     v += dpp_f64<0xB1>(v);
@@ -145,7 +126,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_tokens(const void* 
     }
     const double at = (double)pos + (double)(w.shift ? w.shift[b] : 0);
     for (int i = threadIdx.x; i < s.rotary >> 1; i += kThreads) turns[i] = turn_of(at, inv_freq[i]);
-    if (w.norm && turned) squares[threadIdx.x] = squares_of<kBf16, double>(slot.own, D - d0);
+    if (w.norm && turned) squares[threadIdx.x] = squares_of<kBf16>(slot.own, D - d0);
     __syncthreads();
     if (!mine) return;
     float x[8], none[8];
@@ -193,8 +174,9 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_tokens(const void* 
 // stand in kLanes neighbouring lanes of a wave, which add up their squares without LDS; a thread keeps its tokens and dims over the heads, so that
 // sines and cosines are computed once.  Values are turned over through LDS: the cache holds eight tokens of a dim together.
 //
-// Bound by memory: two prompts of 2000 tokens, 64 heads of 128 over 8, 46 us, 3.6 TB/s (the same without norms 42).  Gains come from LDS (in 16 registers more
-// 62, as fewer waves fit); sums of squares in 64 bits throughout: 47, and 17.9 instead of 16.4 on ragged prompts of 41 MB, 32 heads of 100.
+// Bound by memory: two prompts of 2000 tokens, 64 heads of 128 over 8, 47.5 us, 3.5 TB/s (the same without norms 42).  Gains come from LDS (in 16 registers more
+// 62, as fewer waves fit).  Sums of squares in 32 bits, which lose what is small beside a large element: 46, and 16.4 instead of 17.5 on ragged prompts of
+// 41 MB, 32 heads of 100.
 template <bool kBf16, Turned kTurned, int kLanes>
 __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, NormShape w, KvView kv,
                                                                     RopeShape s, int per, uint16_t* __restrict__ q) {
@@ -215,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
     const int u0 = blockIdx.y * per, u1 = min(u0 + per, units);
     const int page_index = blk >= 0 ? blk / kv.page_blocks : 0, page = blk >= 0 ? kv.table[b * kv.table_stride + page_index] : -1;
     const double shift = w.shift ? (double)w.shift[b] : 0.0;
-    const float inv_d = 1.0f / D;
+    const double inv_d = 1.0 / D;
     const int half = s.rotary >> 1, half8 = (half + 7) >> 3, slots = slots_of<kTurned>(D, s);
     const int j = threadIdx.x & (kLanes - 1);
     const int d0 = kTurned == Turned::Split && j >= half8 ? s.rotary + 8 * (j - half8) : 8 * j;
@@ -260,20 +242,12 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
         for (int m = 0; m < kM; ++m) {
             float r = 1.0f;
             if (w.norm && (query || key)) {                    // all lanes: the sum goes over neighbours
-                auto squares = [&](auto zero) {
-                    auto sum = zero;
-                    if (tok[m] >= 0) {
-                        sum = squares_of<kBf16, decltype(zero)>(slot[m].own, D - d0);
-                        if (both) sum += squares_of<kBf16, decltype(zero)>(slot[m].low, 8);
-                    }
-                    return lanes_sum<kLanes>(sum);
-                };
-                const float sum = squares(0.0f);
-                r = head_scale(sum, inv_d, w.eps);
-                if (__builtin_amdgcn_ballot_w64(tok[m] >= 0 && !in_range(sum))) {
-                    const float far = head_scale(squares(0.0), 1.0 / D, w.eps);
-                    if (!in_range(sum)) r = far;
+                double sum = 0.0;
+                if (tok[m] >= 0) {
+                    sum = squares_of<kBf16>(slot[m].own, D - d0);
+                    if (both) sum += squares_of<kBf16>(slot[m].low, 8);
                 }
+                r = head_scale(lanes_sum<kLanes>(sum), inv_d, w.eps);
             }
             if (tok[m] < 0) continue;
             const int64_t out = ((int64_t)(row0 + tok[m]) * s.heads + u) * D;
