@@ -571,7 +571,8 @@ bitnet_status bitnet_attention_prefill(const void* q, const bitnet_kv* kv, int64
 
 /*
  * bitnet_rope_kv_append with a norm of every query and key head in front, in the same pass: x -> x / sqrt(mean(x^2) + eps) * gain over the head's dims,
- * then the turn.  Values are not normed.  The mean of the squares is fp64, everything behind it fp32, the result rounded once; a head of zeros stays zeros.
+ * then the turn.  Values are not normed.  The mean of the squares is fp64, everything behind it fp32, the result rounded once; a head of zeros stays zeros, and
+ * of one with an infinity the finite dims become zeros, the others (in front of the turn) NaN.
  *   norm            0: no norm (the gains and eps are ignored)
  *   q_gain, k_gain  [head_dim] float (device), one for all heads of queries and of keys, or NULL for no gain
  *   eps             >= 0 and finite (BITNET_ERR_SHAPE otherwise)

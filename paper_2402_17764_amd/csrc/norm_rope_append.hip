@@ -17,11 +17,13 @@ struct NormShape {
     int norm;                          // 0: heads are turned as they are
 };
 
-// 1 / sqrt(mean + eps): the 64-bit instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is.
+// 1 / sqrt(mean + eps): the 64-bit instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is; of one with an infinity (its sum in
+// 64 bits has no other way to be one) the finite dims become zeros and the others NaN.
 __device__ inline float head_scale(double sum, double inv_d, float eps) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const double a = __builtin_fma(sum, inv_d, (double)eps);
     if (!(sum > 0.0)) return sum == 0.0 ? 0.0f : (float)sum;           // NaN stays
+    if (sum == __builtin_inf()) return 0.0f;
     const double y = __builtin_amdgcn_rsq(a);
     return (float)(y * __builtin_fma(-0.5 * a, y * y, 1.5));
 #else

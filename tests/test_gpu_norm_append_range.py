@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from attention_ref import F32_HALF_STEP
+from attention_ref import F32_HALF_STEP, bf16
 from test_gpu_attention import dev, host
 
 pytestmark = pytest.mark.gpu
@@ -16,14 +16,15 @@ def nearest_bf16(x):
     return np.ldexp(np.rint(m * 256.0), e - 8)
 
 
-def append(gpu_lib, x, D, one, q_gain=None, eps=0.0, freq=None, k_gain=None):
-    """x [n, 3, D] fp32: a query, a key and a value head of n sequences' first tokens -> (queries [n, D], keys [n, D]) on the host."""
+def append(gpu_lib, x, D, one, q_gain=None, eps=0.0, freq=None, k_gain=None, pairs=False, f32=True):
+    """x [n, 3, D]: a query, a key and a value head of n sequences' first tokens -> (queries [n, D], keys [n, D]) on the host."""
     n = len(x)
     k, v = gpu_lib.kv_cache(n, 32, 1, D)
     k.fill_(1.0), v.fill_(1.0)
     as_dev = lambda a: None if a is None else dev(a, np.float32)  # noqa: E731
-    q = gpu_lib.norm_rope_kv_append(dev(x.reshape(n, -1), np.float32), as_dev(freq), k, v, torch.arange(n, device="cuda", dtype=torch.int32).view(n, 1), dev(np.ones(n)), 1,
-                                    as_dev(q_gain), as_dev(k_gain), eps, q_start=None if one else dev(np.arange(n + 1)))
+    qkv = dev(x.reshape(n, -1), np.float32).to(torch.float32 if f32 else torch.bfloat16)
+    q = gpu_lib.norm_rope_kv_append(qkv, as_dev(freq), k, v, torch.arange(n, device="cuda", dtype=torch.int32).view(n, 1), dev(np.ones(n)), 1,
+                                    as_dev(q_gain), as_dev(k_gain), eps, q_start=None if one else dev(np.arange(n + 1)), pairs=pairs)
     return host(q)[:, 0], host(k)[:, 0, 0, :, 0].reshape(n, -1)[:, :D]
 
 
@@ -45,3 +46,31 @@ def test_sums_of_squares_are_64_bits(gpu_lib, one, D, turned):
         y = x[:, i].astype(np.float64)
         y = np.abs(y / np.sqrt((y * y).mean(axis=1, keepdims=True)) * gain.astype(np.float64))
         assert np.all(np.abs(got) >= nearest_bf16(y * (1 - 3.01 * F32_HALF_STEP))) and np.all(np.abs(got) <= nearest_bf16(y * (1 + 3.01 * F32_HALF_STEP)))
+
+
+@pytest.mark.parametrize("one", [False, True])
+@pytest.mark.parametrize("D", [8, 64, 100, 128, 256])
+@pytest.mark.parametrize("turned", [None, "halves", "pairs"])
+@pytest.mark.parametrize("f32", [False, True])
+def test_heads_with_infinities(gpu_lib, one, D, turned, f32):
+    """x / inf: zeros in the finite dims, no number in the others, nor in what they are turned with; a head that is no number somewhere is none anywhere.  The heads
+    beside them are what they are without."""
+    rng = np.random.default_rng(D)
+    x = bf16(rng.standard_normal((5, 3, D)))
+    plain = append(gpu_lib, x, D, one, eps=1e-6, freq=None if turned is None else np.ones(D // 2), pairs=turned == "pairs", f32=f32)
+    marks = {(0, 0): {1: np.inf}, (0, 1): {D - 1: -np.inf}, (1, 0): {0: np.inf, D // 2: -np.inf}, (2, 1): {3: np.nan}, (3, 0): {2: np.inf, 5: np.nan}}
+    for (b, i), at in marks.items():
+        for d, value in at.items():
+            x[b, i, d] = value
+    got = append(gpu_lib, x, D, one, eps=1e-6, freq=None if turned is None else np.ones(D // 2), pairs=turned == "pairs", f32=f32)
+    for b in range(5):
+        for i in range(2):
+            at = marks.get((b, i))
+            if at is None:
+                assert np.array_equal(got[i][b], plain[i][b])
+                continue
+            if any(np.isnan(value) for value in at.values()):
+                assert np.isnan(got[i][b]).all()
+                continue
+            none = set(at) if turned is None else set(at) | {d ^ 1 if turned == "pairs" else (d + D // 2) % D for d in at}
+            assert np.isnan(got[i][b][sorted(none)]).all() and (np.delete(got[i][b], sorted(none)) == 0).all()
