@@ -19,15 +19,18 @@ struct NormShape {
 
 // 1 / sqrt(mean + eps): the 64-bit instruction's 2^-23 and one Newton step.  A head of zeros stays zeros, whatever eps is; of one with an infinity (its sum in
 // 64 bits has no other way to be one) the finite dims become zeros and the others NaN.
-__device__ inline float head_scale(double sum, double inv_d, float eps) {
+struct HeadScale { float first, then; };   // two factors: of heads whose elements are near either end of fp32's range the one would not be a normal number
+__device__ inline HeadScale head_scale(double sum, double inv_d, float eps) {
 #if defined(__HIP_DEVICE_COMPILE__)
     const double a = __builtin_fma(sum, inv_d, (double)eps);
-    if (!(sum > 0.0)) return sum == 0.0 ? 0.0f : (float)sum;           // NaN stays
-    if (sum == __builtin_inf()) return 0.0f;
-    const double y = __builtin_amdgcn_rsq(a);
-    return (float)(y * __builtin_fma(-0.5 * a, y * y, 1.5));
+    const double y = __builtin_amdgcn_rsq(a), r = y * __builtin_fma(-0.5 * a, y * y, 1.5);
+    if (r >= 0x1p-64 && r <= 0x1p64 && sum > 0.0) return {1.0f, (float)r};
+    if (!(sum > 0.0)) return {1.0f, sum == 0.0 ? 0.0f : (float)sum};   // NaN stays
+    if (sum == __builtin_inf()) return {1.0f, 0.0f};
+    if (r > 1.0) return {0x1p64f, (float)(r * 0x1p-64)};                // elements below 2^-60: exact
+    return {0x1p-64f, (float)(r * 0x1p64)};
 #else
-    return 0.0f;
+    return {};
 #endif
 }
 
@@ -62,19 +65,26 @@ __device__ inline void gains_of(float (&g)[8], const float* gain, int d, int end
 
 // Eight dims from d0 on of a head, with their partners' raw values (Split: of the lower half; Any: those in front and behind) and all gains, turned.
 template <bool kBf16, Turned kTurned>
-__device__ inline void norm_and_turn(float (&x)[8], float (&y)[8], const Slot<kBf16, kTurned>& v, int d0, float r, const float (&g)[8], const float (&partner)[8],
+__device__ inline void norm_and_turn(float (&x)[8], float (&y)[8], const Slot<kBf16, kTurned>& v, int d0, HeadScale r, const float (&g)[8], const float (&partner)[8],
                                      const Turn (&t)[8], const RopeShape& s) {
     const int half = s.rotary >> 1;
-    floats_of<kBf16>(x, v.own);
+    auto scale = [&](float (&z)[8], const float (&gains)[8]) {
+        if (__builtin_amdgcn_ballot_w64(r.first != 1.0f))
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
+            for (int e = 0; e < 8; ++e) z[e] *= r.first;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = z[e] * r.then * gains[e];
+    };
+    floats_of<kBf16>(x, v.own);
+    scale(x, g);
     if constexpr (kTurned == Turned::Split) {
         if (d0 >= half) return;
         floats_of<kBf16>(y, v.low);
+        scale(y, partner);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float b = y[e] * r * partner[e], a = x[e] * t[e].cos - b * t[e].sin;
-            y[e] = b * t[e].cos + x[e] * t[e].sin;
+            const float a = x[e] * t[e].cos - y[e] * t[e].sin;
+            y[e] = y[e] * t[e].cos + x[e] * t[e].sin;
             x[e] = a;
         }
     } else if constexpr (kTurned == Turned::Pairs) {
@@ -90,8 +100,11 @@ __device__ inline void norm_and_turn(float (&x)[8], float (&y)[8], const Slot<kB
         floats_of<kBf16>(l, v.low);
         floats_of<kBf16>(h, v.high);
 #pragma unroll
+        for (int e = 0; e < 8; ++e) l[e] = d0 + e < half ? -l[e] : h[e];
+        scale(l, partner);
+#pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (d0 + e < s.rotary) x[e] = x[e] * t[e].cos + (d0 + e < half ? -l[e] : h[e]) * r * partner[e] * t[e].sin;
+            if (d0 + e < s.rotary) x[e] = x[e] * t[e].cos + l[e] * t[e].sin;
     }
 }
 // the gains of eight dims and of their partners
@@ -133,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_tokens(const void* 
     if (!mine) return;
     float x[8], none[8];
     if (turned) {
-        float r = 1.0f;
+        HeadScale r{1.0f, 1.0f};
         if (w.norm) {
             double sum = 0.0;
             for (int i = 0; i < quads; ++i) sum += squares[threadIdx.x - j + i];
@@ -172,15 +185,20 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_tokens(const void* 
     }
 }
 
+// Waves that have to fit on a SIMD: pairs of bf16 that miss one by two registers cost 10 %.
+constexpr int norm_waves(bool bf16, Turned turned, int lanes) {
+    return !bf16 || turned != Turned::Pairs ? 1 : lanes == 8 ? 8 : lanes == 16 ? 6 : 4;
+}
+
 // Runs of new tokens: a workgroup takes the new tokens of one cache block (32 positions) and `per` heads of their rows.  The slots of a head of a token
 // stand in kLanes neighbouring lanes of a wave, which add up their squares without LDS; a thread keeps its tokens and dims over the heads, so that
 // sines and cosines are computed once.  Values are turned over through LDS: the cache holds eight tokens of a dim together.
 //
-// Bound by memory: two prompts of 2000 tokens, 64 heads of 128 over 8, 47.5 us, 3.5 TB/s (the same without norms 42).  Gains come from LDS (in 16 registers more
-// 62, as fewer waves fit).  Sums of squares in 32 bits, which lose what is small beside a large element: 46, and 16.4 instead of 17.5 on ragged prompts of
+// Bound by memory: two prompts of 2000 tokens, 64 heads of 128 over 8, 47.8 us, 3.5 TB/s (the same without norms 42).  Gains come from LDS (in 16 registers more
+// 62, as fewer waves fit).  Sums of squares in 32 bits, which lose what is small beside a large element: 46, and 16.4 instead of 17.7 on ragged prompts of
 // 41 MB, 32 heads of 100.
 template <bool kBf16, Turned kTurned, int kLanes>
-__global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, NormShape w, KvView kv,
+__global__ __launch_bounds__(kThreads, norm_waves(kBf16, kTurned, kLanes)) void norm_rope_append_blocks(const void* __restrict__ qkv, const float* __restrict__ inv_freq, NormShape w, KvView kv,
                                                                     RopeShape s, int per, uint16_t* __restrict__ q) {
     constexpr int kM = kLanes / 8, kTokens = kThreads / kLanes, kPitch = 256 + 8;      // tokens of a workgroup at a time
     __shared__ uint4 tile4[kKvBlock * kPitch / 8];
@@ -242,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_append_blocks(const void* 
         const int64_t at = (int64_t)block * kKvBlock * Dp;
 #pragma unroll
         for (int m = 0; m < kM; ++m) {
-            float r = 1.0f;
+            HeadScale r{1.0f, 1.0f};
             if (w.norm && (query || key)) {                    // all lanes: the sum goes over neighbours
                 double sum = 0.0;
                 if (tok[m] >= 0) {

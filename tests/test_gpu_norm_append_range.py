@@ -74,3 +74,25 @@ def test_heads_with_infinities(gpu_lib, one, D, turned, f32):
                 continue
             none = set(at) if turned is None else set(at) | {d ^ 1 if turned == "pairs" else (d + D // 2) % D for d in at}
             assert np.isnan(got[i][b][sorted(none)]).all() and (np.delete(got[i][b], sorted(none)) == 0).all()
+
+
+@pytest.mark.parametrize("one", [False, True])
+@pytest.mark.parametrize("size", [3e38, 1e25, 1e-19, 1e-30, 1e-37, 1e-39, 1e-41, 3e-44])
+@pytest.mark.parametrize("turned", [None, "halves", "pairs"])
+@pytest.mark.parametrize("f32", [False, True])
+def test_heads_near_both_ends_of_the_range(gpu_lib, one, size, turned, f32):
+    """Without eps a head of any size comes out as one of size one: the factor is rounded once, to fp32, and the two products are (a power of two in front of them
+    changes nothing): 3 half steps, at position 0."""
+    rng = np.random.default_rng(3)
+    n, D = 1000, 128 if turned != "halves" else 100
+    x = (rng.uniform(0.3, 1.0, (n, 3, D)) * rng.choice([-1.0, 1.0], (n, 3, D)) * size).astype(np.float32).astype(np.float64)
+    if not f32:
+        x = bf16(x)
+    gains = [rng.uniform(0.5, 2.0, D).astype(np.float32) for _ in range(2)]
+    got = append(gpu_lib, x, D, one, gains[0], 0.0, None if turned is None else np.ones(D // 2), gains[1], turned == "pairs", f32)
+    for i, gain in enumerate(gains):
+        y, some = x[:, i], x[:, i].any(axis=1)
+        y = np.abs(y[some] / np.sqrt((y[some] * y[some]).mean(axis=1, keepdims=True)) * gain.astype(np.float64))
+        assert some.any() or not f32
+        assert np.all(np.abs(got[i][some]) >= nearest_bf16(y * (1 - 3.01 * F32_HALF_STEP))) and np.all(np.abs(got[i][some]) <= nearest_bf16(y * (1 + 3.01 * F32_HALF_STEP)))
+        assert (got[i][~some] == 0).all()
