@@ -85,11 +85,12 @@ struct ColumnArgs {
     const uint16_t* q;
     const float* state;                // [T][heads][2]: m, l
     float* weights;                    // [B][kv heads][stride]
-    float* parts;                      // [tasks][keys of a tile]
-    int64_t stride, tasks;             // of the weights: tiles of keys times splits times sequences times kv heads
+    float* parts;                      // [shares][sequences times kv heads][keys of a tile]
+    int64_t stride, tasks;             // of the weights: tiles of keys, or shares of them, times sequences times kv heads
     float scale;
     int heads, group, T;
-    int splits, least;                 // workgroups that share a tile's rows, at most, and stages that one has at least
+    uint32_t shares, most;             // of a sequence's tiles for one head, together, that the parts have room for; workgroups that share a tile's rows, at most
+    int least;                         // stages that one has at least
     uint32_t magic, shift;             // of the division by `group`: the quotient of n is (high word of n magic + n) >> shift, n below 2^31
     __device__ int token(int row) const { return (int)((__umulhi((uint32_t)row, magic) + (uint32_t)row) >> shift); }
 };
@@ -112,15 +113,19 @@ struct ColumnTile {
         : ColumnTile(a, kv, task, (uint32_t)(kv.B * kv.kv_heads), each_of(task, (uint32_t)(kv.B * kv.kv_heads))) {}
     __device__ ColumnTile(const ColumnArgs& a, const KvView& kv, int64_t task, uint32_t pairs, uint32_t each)
         : h((int)((uint32_t)(task - (int64_t)each * pairs) % (uint32_t)kv.kv_heads)), b((int)((uint32_t)(task - (int64_t)each * pairs) / (uint32_t)kv.kv_heads)),
-          share((int)(each % (uint32_t)a.splits)), tile((int)(each / (uint32_t)a.splits)), nt(kv, b, a.T) {
+          nt(kv, b, a.T) {
         blocks = blocks_of(kv, b);
+        // as many shares of a tile as the sequence's tiles leave, whatever its table has room for
+        const uint32_t tiles = ((uint32_t)blocks + 4 * Columns<kC>::kKB - 1) / (4 * Columns<kC>::kKB), splits = min(max(a.shares / max(tiles, 1u), 1u), a.most);
+        tile = (int)(each / splits);
+        share = (int)(each - (uint32_t)tile * splits);
         blk = tile * (4 * Columns<kC>::kKB);
         j0 = blk * kKvBlock;
         rows = nt.n * a.group;
         if (nt.n == 0 || blk >= blocks) { stages = 0, run = 1, first = 0; return; }
         first = max(j0 - nt.pos0, 0) * a.group / 16 * 16;
         stages = (rows - first + Columns<kC>::kRows - 1) / Columns<kC>::kRows;
-        run = max((stages + a.splits - 1) / a.splits, a.least);
+        run = max((stages + (int)splits - 1) / (int)splits, a.least);
     }
 };
 
@@ -314,19 +319,24 @@ __global__ __launch_bounds__(Columns<kC>::kKeys) void attention_weights_join(Col
 // How many workgroups share the rows of a tile of keys: as many as make 1024 of them, two rounds of what the chip holds, with two stages or more each;
 // their sums go through the workspace and another launch (us without that launch, 1 / 2 / 4 / 8 / 16 / 32: 64 heads over 8, 512 tokens 110 / 70 / 37 / 21 / 13 /
 // 8.8, 2048 tokens 351 / 192 / 112 / 81 / 73 / -; 40 heads, 2048 tokens 57 / 46 / 49 / 50 / 57 / -; six of 450 behind 250, 32 heads of 100 36 / 38 / 42 / 54 / 66 / -).
+// A sequence's tiles are counted where its length is known, on the device, and not by the room in the tables (64 heads over 8 in a table of 32768 tokens, whole
+// calls: 512 tokens 31.5 us, by the room 110; 2048 tokens 152, by the room 430); here stands what all of them may be together.  Where tables have more than four
+// times the call's tokens the other launch, 4 us, is there whether tiles are shared or not; where they have less, only if they are by the room.
 struct ColumnsPlan {
     int64_t tasks;
-    int splits;
+    int shares, most;                  // as in ColumnArgs
     size_t bytes;
 };
 constexpr int kLeastStages = 2;
 template <int kC>
 ColumnsPlan columns_plan(const KvView& kv, int64_t T, int group) {
     using Shape = Columns<kC>;
-    const int64_t tiles = (int64_t)kv.B * kv.kv_heads * ceil_div(kv.max_blocks, 4 * Shape::kKB), most = ceil_div(T * group, Shape::kRows * kLeastStages);
-    int64_t n = tiles < 1024 ? 1024 / tiles : 1;
-    n = n < most ? n : most;
-    return {tiles * n, (int)n, n < 2 ? 0 : (size_t)(tiles * n * Shape::kKeys) * 4};
+    const int64_t pairs = (int64_t)kv.B * kv.kv_heads, room = ceil_div(kv.max_blocks, 4 * Shape::kKB), most = ceil_div(T * group, Shape::kRows * kLeastStages);
+    const bool roomy = (int64_t)kv.max_blocks * kKvBlock > 4 * (T / kv.B);
+    int64_t shares = 1024 / pairs;
+    if (most < 2 || shares < 2 || (!roomy && shares / room < 2)) return {pairs * room, 1, 1, 0};
+    if (shares / most >= room) shares = room * most;
+    return {pairs * (room > shares ? room : shares), (int)shares, (int)(most < shares ? most : shares), (size_t)(pairs * shares * Shape::kKeys) * 4};
 }
 
 // Splits of single tokens' rows and the workspace: parts, then scores.
@@ -406,12 +416,14 @@ hipError_t launch_attention_prefill_weights(const void* q, const KvView& kv, int
         int shift = 0;
         while ((1 << shift) < group) ++shift;
         const ColumnArgs a{static_cast<const uint16_t*>(q), keep.state, weights, reinterpret_cast<float*>(at + plan.states), stride, p.tasks, scale * 1.44269504f,
-                           heads, group, (int)T, p.splits, kLeastStages, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - group)) / group + 1), (uint32_t)shift};
+                           heads, group, (int)T, (uint32_t)p.shares, (uint32_t)p.most, kLeastStages, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - group)) / group + 1), (uint32_t)shift};
         const unsigned blocks = (unsigned)(p.tasks < kMostBlocks ? p.tasks : kMostBlocks);
         attention_weights_of_runs<c.value, exact.value><<<blocks, 256, 0, stream>>>(a, kv);
         const hipError_t ran = hipGetLastError();
-        if (ran != hipSuccess || p.splits < 2) return ran;
-        attention_weights_join<c.value><<<blocks, Columns<c.value>::kKeys, 0, stream>>>(a, kv);
+        if (ran != hipSuccess || p.bytes == 0) return ran;
+        ColumnArgs join = a;
+        join.tasks = (int64_t)kv.B * kv.kv_heads * p.shares;             // at most 1024
+        attention_weights_join<c.value><<<(unsigned)join.tasks, Columns<c.value>::kKeys, 0, stream>>>(join, kv);
         return hipGetLastError();
     });
 }
