@@ -630,7 +630,8 @@ bitnet_status bitnet_attention_prefill_weights(const void* q, const bitnet_kv* k
  *   table_out       [B] rows of int32 page numbers (device), table_out_stride apart, with room for min(keep, max_pages*page_tokens) tokens.  None may be a
  *                   page that a sequence of the call has its tokens on, none be named twice.  On a page that is not there nothing is stored; a token from
  *                   a page that is not there is zeros.
- *   weights_out     [B][kv_heads] rows of weights_out_stride floats, >= min(keep, max_pages*page_tokens); `weights` itself, with its stride, is allowed
+ *   weights_out     [B][kv_heads] rows of weights_out_stride floats, >= min(keep, max_pages*page_tokens); `weights` itself, with its stride, is allowed.  The
+ *                   weights as they were, but for -0, which comes out as 0, and NaN, which comes out as one NaN
  *   kv_len_out      [B] int32: min(length, keep); kv_len itself is allowed
  *   kept            [B][kv_heads][keep] int32: the old positions; entries from kv_len_out[b] on are left as they were
  *   kv->v, kv->k are read and written; kv->q_start is not read.  Two launches.
