@@ -30,13 +30,13 @@ __global__ __launch_bounds__(256) void attention_join(JoinArgs a, Parts parts, K
     const int n = splits_of(a, parts, kv, t, head);
     if (n < 2) return;                                      // stored by the workgroup that had all of it
     if constexpr (kKeep) {
-        const JoinState all = join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, n, 0, a.scale, kv.D, a.o, blockIdx.x);
+        const JoinState all = join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, a.scale, kv.D, a.o, blockIdx.x);
         if (threadIdx.x == 0) {
             keep.state[2 * (int64_t)blockIdx.x] = all.top;
             keep.state[2 * (int64_t)blockIdx.x + 1] = all.total;
         }
     } else {
-        join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, n, 0, a.scale, kv.D, a.o, blockIdx.x);
+        join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, a.scale, kv.D, a.o, blockIdx.x);
     }
 }
 

@@ -26,22 +26,21 @@ struct JoinRoom {
 };
 struct JoinState { float top, total; };                    // m and l of the row
 
-// Joins the `n` splits of row `row`, of which the first `near` stand at places place0, place0 + 1, ... and the others from place0 + far on.
+// Joins the `n` splits of row `row`, which stand at places place0, place0 + 1, ...
 template <bool kF32>
-__device__ inline JoinState join_row(JoinRoom& room, const Parts& parts, int64_t place0, int n, int near, int far, float scale, int D, void* o, int64_t row) {
+__device__ inline JoinState join_row(JoinRoom& room, const Parts& parts, int64_t place0, int n, float scale, int D, void* o, int64_t row) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), dim = 4 * lane;
-    auto place = [&](int s) { return place0 + (s < near ? s : far + (s - near)); };
     auto sums_of = [&](int s) {
         v4f y = {0, 0, 0, 0};
-        const float* p = parts.sums + place(s) * D + dim;
+        const float* p = parts.sums + (place0 + s) * D + dim;
         if (dim + 4 <= D) __builtin_memcpy(&y, p, 16);
         else if (dim < D) { y[0] = p[0]; y[1] = p[1]; }     // heads have an even number of dims
         return y;
     };
     float m = kMinusInf, l = 0.0f;                          // one split a thread: its weight, exp(m_s - m), and its share of l
     if ((int)threadIdx.x < n) {
-        m = parts.state[place(threadIdx.x) * 2];
-        l = parts.state[place(threadIdx.x) * 2 + 1];
+        m = parts.state[(place0 + threadIdx.x) * 2];
+        l = parts.state[(place0 + threadIdx.x) * 2 + 1];
     }
     float top = wave_max(m);
     if (lane == 0) room.tops[wave] = top;

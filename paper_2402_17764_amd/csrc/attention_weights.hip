@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void attention_weights_of_tokens(void* o, Weig
     if ((int)blockIdx.x < a.joins) {
         const int b = blockIdx.x / a.heads, blocks = blocks_of(kv, b), run = parts.run(blocks), n = (blocks + run - 1) / run;
         if (n < 2) return;                                  // stored by the workgroup that had all of it
-        join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, n, 0, a.scale, kv.D, o, blockIdx.x);
+        join_row<kF32>(room, parts, (int64_t)blockIdx.x * parts.splits, n, a.scale, kv.D, o, blockIdx.x);
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
