@@ -27,7 +27,7 @@ struct SharedPlan {
 // are launches (us, one launch / two: 13 sequences behind 1500 tokens, 32 heads 20.1 / 25.5; 6 behind 8000, 64 heads over 8 22.5 / 24.7; 16 behind 16000
 // 37.2 / 38.7, 20 45.2 / 40.5; 30 behind 16000, 28 over 4 42.5 / 41.0; 48 behind 24000, 64 over 8 135 / 115).  Two launches, and 256 rows: tiles of 128, which halve what comes
 // through LDS (the last one 110; 30 behind 16000, which has 210, 44.8).  The shared keys are split until there are two workgroups for each CU, a sequence's own until there
-// are four or five, with 256 tokens each or more (48 behind 24000, own ones in a workgroup each: 46 us for them, split 39; shared ones to three workgroups a CU 110).
+// are four or five, with 256 tokens each or more (48 behind 24000, own ones in a workgroup each: 46 us for them, split 39; shared ones to three workgroups a CU 116 instead of 110).
 SharedPlan shared_plan(const KvView& kv, int groups, int heads, bool f32) {
     const int group = heads / kv.kv_heads;
     const int64_t capacity = (int64_t)kv.max_blocks * kKvBlock, rows = ceil_div((int64_t)kv.B * group, groups), most = ceil_div(capacity, 256);

@@ -20,8 +20,8 @@ struct WeightsArgs {
 constexpr int kChunk = 1024;
 
 // Joins the rows that several workgroups shared, one to a workgroup, then turns chunks of scores into weights, four tokens a thread.  Bound by memory: three
-// sequences of 20000 to 49152 tokens, 64 heads over 8, 31 MB of scores in 9.5 us.  What scores cost more is that they are written beside the stream of the
-// cache (there 80 us with them, 66 without; with streaming stores 85).
+// sequences of 20000 to 49152 tokens, 64 heads over 8, 31 MB of scores in 9.7 us.  What scores cost more is that they are written beside the stream of the
+// cache (there 83 us with them, 66 without; with streaming stores 87).
 template <bool kF32>
 __global__ __launch_bounds__(256) void attention_weights_of_tokens(void* o, WeightsArgs a, Parts parts, KvView kv) {
     __shared__ JoinRoom room;
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(Columns<kC>::kKeys) void attention_weights_join(Col
 // their sums go through the workspace and another launch (us without that launch, 1 / 2 / 4 / 8 / 16 / 32: 64 heads over 8, 512 tokens 110 / 70 / 37 / 21 / 13 /
 // 8.8, 2048 tokens 351 / 192 / 112 / 81 / 73 / -; 40 heads, 2048 tokens 57 / 46 / 49 / 50 / 57 / -; six of 450 behind 250, 32 heads of 100 36 / 38 / 42 / 54 / 66 / -).
 // A sequence's tiles are counted where its length is known, on the device, and not by the room in the tables (64 heads over 8 in a table of 32768 tokens, whole
-// calls: 512 tokens 31.5 us, by the room 110; 2048 tokens 152, by the room 430); here stands what all of them may be together.  Where tables have more than four
+// calls: 512 tokens 31.5 us, by the room 110); here stands what all of them may be together.  Where tables have more than four
 // times the call's tokens the other launch, 4 us, is there whether tiles are shared or not; where they have less, only if they are by the room.
 struct ColumnsPlan {
     int64_t tasks;

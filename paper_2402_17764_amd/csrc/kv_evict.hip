@@ -5,9 +5,9 @@
 // unsigned image of the float that keeps the order), by counts in LDS; then the positions above it, and of those equal to it the first ones, are
 // numbered by a running sum.  Second launch: the tokens of a block of the new pages to a workgroup.
 //
-// Measured on five sequences of 20000 to 40000 tokens, 8 heads of 128, cut to 8000: the choice 38 us, bound by one CU's instructions and LDS (a pass over 30000
-// weights 6, numbering and writing 8000 positions 13); the move 142, bound by memory, as a token's dims share 128-byte lines with the tokens
-// around it: 581 MB read for the 164 that stay, 5.2 TB/s.
+// Measured on five sequences of 20000 to 40000 tokens, 8 heads of 128, cut to 8000: the choice 41 us, bound by one CU's instructions and LDS (a pass over 30000
+// weights 6, numbering and writing 8000 positions 13); the move 145, bound by memory, as a token's dims share 128-byte lines with the tokens
+// around it: 581 MB read for the 164 that stay, 5.1 TB/s.
 #include "bitnet_device.hpp"
 #include "bitnet_internal.hpp"
 #include "kv_layout.hpp"
