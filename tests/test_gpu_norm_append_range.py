@@ -96,3 +96,23 @@ def test_heads_near_both_ends_of_the_range(gpu_lib, one, size, turned, f32):
         assert some.any() or not f32
         assert np.all(np.abs(got[i][some]) >= nearest_bf16(y * (1 - 3.01 * F32_HALF_STEP))) and np.all(np.abs(got[i][some]) <= nearest_bf16(y * (1 + 3.01 * F32_HALF_STEP)))
         assert (got[i][~some] == 0).all()
+
+
+@pytest.mark.parametrize("D", [8, 64, 100, 128, 256])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("f32", [False, True])
+def test_a_row_of_a_prompt_is_the_token(gpu_lib, D, pairs, f32):
+    """The same bits from both kernels: sums of squares in 64 bits differ by their order in 2^-50 of them, which reaches the factor's rounding to 24 bits
+    in one of 2^26 heads."""
+    rng = np.random.default_rng(D)
+    n, heads, kv_heads = 1500, 4, 2
+    x = rng.standard_normal((n, (heads + 2 * kv_heads) * D)) * np.exp(rng.standard_normal((n, 1)))
+    qkv = dev(x, np.float32).to(torch.float32 if f32 else torch.bfloat16)
+    freq, gains = dev(10000.0 ** (-np.arange(0, D, 2) / D), np.float32), [dev(rng.uniform(0.5, 2.0, D), np.float32) for _ in range(2)]
+    table, lens = torch.arange(n, device="cuda", dtype=torch.int32).view(n, 1), dev(rng.integers(1, 33, n))
+    got = []
+    for start in (None, dev(np.arange(n + 1))):
+        k, v = gpu_lib.kv_cache(n, 32, kv_heads, D)
+        k.zero_(), v.zero_()
+        got.append((gpu_lib.norm_rope_kv_append(qkv, freq, k, v, table, lens, heads, *gains, q_start=start, pairs=pairs), k, v))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
